@@ -443,6 +443,115 @@ void            patdnn_stack_destroy(patdnn_stack_t s);     /* NULL is a no-op *
  */
 patdnn_status_t patdnn_stack_run_static(patdnn_stack_t s, const float* input, float* output,   /* DEVICE */
                                         void* stream);
+/*
+ * ---------------------------------------------------------------------------------------------
+ * What stands between and behind the 3x3 convolutions of a network: the order of channels, group
+ * normalisation, and linear layers (pointwise convolutions are linear layers whose rows are pixels) on
+ * weights of four bits.  No handles: all memory is the caller's, every call is asynchronous on
+ * `stream`, allocates nothing and never synchronises.  Outputs must not overlap inputs, counted from a tensor's first
+ * to its last element.  All pointers DEVICE and aligned to their elements unless said otherwise.
+ * ---------------------------------------------------------------------------------------------
+ */
+
+/* Element types of activations.  Sums and statistics are fp32 whatever the type; a result is rounded
+ * to its type once, to the nearest, ties to even. */
+#define PATDNN_F32   0
+#define PATDNN_F16   1     /* IEEE binary16 */
+#define PATDNN_BF16  2     /* bfloat16 */
+#define PATDNN_MXFP4 3     /* codes of patdnn_mxfp4_quantize, where a call says that it takes them */
+
+/* Activations. */
+#define PATDNN_ACT_NONE 0
+#define PATDNN_ACT_RELU 1  /* z where z > 0, 0 where z <= 0; NaN stays NaN */
+#define PATDNN_ACT_SILU 2  /* z / (1 + exp(-z)) */
+
+/*
+ * Order of channels, with a change of type: `channels` x `pixels` matrices of `n` images, transposed.
+ *   patdnn_channels_last   input [n][channels][pixels], dense; output [n][pixels][channels] with
+ *       `out_image` / `out_pixel` elements from image to image and pixel to pixel, so that it may be a
+ *       slice of the channels of a wider tensor (out_pixel >= channels, out_image >= one image)
+ *   patdnn_channels_first  the inverse: input with strides (>= 0), output dense
+ * n == 0 is a no-op.
+ */
+patdnn_status_t patdnn_channels_last(const void* input, int32_t in_type, int32_t n, int32_t channels, int32_t pixels,
+                                     void* output, int32_t out_type, int64_t out_image, int64_t out_pixel, void* stream);
+patdnn_status_t patdnn_channels_first(const void* input, int32_t in_type, int64_t in_image, int64_t in_pixel, int32_t n,
+                                      int32_t channels, int32_t pixels, void* output, int32_t out_type, void* stream);
+
+/*
+ * Group norm with an activation, channels last.  Per image and group of channels / groups adjacent
+ * channels, over all pixels (M values): mean, variance = mean of (x - mean)^2, rstd = 1 / sqrt(variance + eps),
+ *   xh = (x - mean) * rstd,  z = gamma[c] * xh + beta[c],  y = act(z).
+ * Backward, with dz = dy * act'(z) (ReLU: 0 where z <= 0):
+ *   dbeta[c] = sum of dz, dgamma[c] = sum of dz * xh, over images and pixels;
+ *   dx = rstd * (gamma dz - (A + xh B) / M), A and B the group's sums of gamma dz and gamma dz xh.
+ * x, y, dy, dx are of `type`, with strides in elements between images and pixels and adjacent channels
+ * (inputs >= 0; outputs: pixels >= channels apart, images >= one image); everything else is fp32:
+ *   gamma, beta   [channels], NULL for ones and zeros
+ *   mean, rstd    [n][groups], outputs of the forward call (NULL: not wanted) and inputs of the backward
+ *                 one.  A group that holds something not finite has NaN outputs.
+ *   dgamma, dbeta [channels] or NULL; written, not added to (zeros for n == 0)
+ *   workspace     patdnn_group_norm_workspace_floats floats, contents undefined before and after
+ * Results repeat bit for bit.  groups divides channels; n == 0 is a no-op but for dgamma and dbeta.
+ */
+typedef struct {
+    int32_t n, pixels, channels, groups;
+    int32_t type;                   /* PATDNN_F32, _F16, _BF16 */
+    int32_t act;
+    float eps;                      /* >= 0; not read by the backward call */
+    int64_t x_image, x_pixel;
+    int64_t y_image, y_pixel;       /* of y; of dx in the backward call */
+    int64_t dy_image, dy_pixel;     /* of dy; not read by the forward call */
+} patdnn_norm_desc_t;
+/* 0 for a description that the call would refuse. */
+size_t patdnn_group_norm_workspace_floats(const patdnn_norm_desc_t* desc, int32_t backward);
+patdnn_status_t patdnn_group_norm(const patdnn_norm_desc_t* desc, const void* x, const float* gamma, const float* beta, void* y,
+                                  float* mean, float* rstd, float* workspace, size_t workspace_floats, void* stream);
+patdnn_status_t patdnn_group_norm_backward(const patdnn_norm_desc_t* desc, const void* dy, const void* x, const float* mean,
+                                           const float* rstd, const float* gamma, const float* beta, void* dx, float* dgamma,
+                                           float* dbeta, float* workspace, size_t workspace_floats, void* stream);
+
+/*
+ * Microscaled 4-bit floating point (MXFP4): 4.25 bits a value.  A row of `cols` values is cut into
+ * blocks of 32 that share a power of two, and stored in whole pieces of 128 values, P = ceil(cols / 128):
+ *   codes   [rows][P * 64] bytes, two values a byte, the earlier one in the low bits: bit 3 the sign, bits 2..0
+ *           select 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Zeros behind the last value.  16-byte aligned.
+ *   scales  [rows][P * 4] bytes: b stands for 2^(b - 127).  4-byte aligned.
+ * Quantising: with a the block's largest magnitude, b = 127 + max(-127, floor(log2 a) - 2) (0 for a block of zeros);
+ * a value becomes the nearest code to value / 2^(b - 127), ties to the even code, magnitudes above 6 become 6.
+ * A block that holds something not finite has b = 255 and zero codes; its values read back as NaN.
+ *   x / out: `type`, `row` elements between rows (out: >= cols), values of a row adjacent.
+ * rows == 0 is a no-op.
+ */
+patdnn_status_t patdnn_mxfp4_quantize(const void* x, int32_t type, int32_t rows, int32_t cols, int64_t row, uint8_t* codes,
+                                      uint8_t* scales, void* stream);
+patdnn_status_t patdnn_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int32_t rows, int32_t cols, void* out,
+                                        int32_t type, int64_t row, void* stream);
+
+/*
+ * Linear layer on MXFP4 weights: out[m][n] = act(bias[n] + sum over k of xq[m][k] * w[n][k]), summed in
+ * fp32.  xq is x quantised as patdnn_mxfp4_quantize does it, within the call; or x holds codes already
+ * (x_type PATDNN_MXFP4, with x_scales).  A pointwise convolution is this layer with the pixels of all
+ * images as rows.
+ *   w, w_scales  patdnn_mxfp4_quantize of the weights [out_features][in_features]
+ *   bias         fp32 [out_features] or NULL
+ *   workspace    patdnn_mxfp4_linear_workspace_bytes bytes, 16-byte aligned (may be NULL if that is 0), contents
+ *                undefined before and after; calls that share one must not overlap in time
+ * Results repeat bit for bit.  rows == 0 is a no-op.
+ */
+typedef struct {
+    int32_t rows, in_features, out_features;
+    int32_t x_type;                 /* PATDNN_F32, _F16, _BF16, _MXFP4 */
+    int32_t out_type;               /* PATDNN_F32, _F16, _BF16 */
+    int32_t act;
+    int64_t x_row;                  /* elements between rows of x, >= 0; not read for PATDNN_MXFP4 */
+    int64_t out_row;                /* >= out_features */
+} patdnn_linear_desc_t;
+size_t patdnn_mxfp4_linear_workspace_bytes(const patdnn_linear_desc_t* desc);
+patdnn_status_t patdnn_mxfp4_linear(const patdnn_linear_desc_t* desc, const void* x, const uint8_t* x_scales, const uint8_t* w,
+                                    const uint8_t* w_scales, const float* bias, void* out, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
 const char* patdnn_status_string(patdnn_status_t s);
 const char* patdnn_last_error(void);
 

@@ -29,8 +29,13 @@ EXPORTS = [
     "patdnn_export_fkw", "patdnn_export_csr", "patdnn_layout_stats", "patdnn_num_variants", "patdnn_variant_name",
     "patdnn_set_config", "patdnn_get_config", "patdnn_tune", "patdnn_tune_ws", "patdnn_tiled_info",
     "patdnn_export_tiled", "patdnn_selftest", "patdnn_destroy",
+    "patdnn_channels_last", "patdnn_channels_first",
+    "patdnn_group_norm", "patdnn_group_norm_backward", "patdnn_group_norm_workspace_floats",
+    "patdnn_mxfp4_quantize", "patdnn_mxfp4_dequantize", "patdnn_mxfp4_linear", "patdnn_mxfp4_linear_workspace_bytes",
     "patdnn_status_string", "patdnn_last_error",
 ]
+PATDNN_F32, PATDNN_F16, PATDNN_BF16, PATDNN_MXFP4 = range(4)
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
 
 
 class LayerDesc(ctypes.Structure):
@@ -70,6 +75,20 @@ class TiledInfo(ctypes.Structure):
 class StackLayer(ctypes.Structure):
     _fields_ = [("layer", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("fuse_relu", ctypes.c_int32),
                 ("pool2", ctypes.c_int32)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("pixels", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("type", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("x_image", ctypes.c_int64), ("x_pixel", ctypes.c_int64),
+                ("y_image", ctypes.c_int64), ("y_pixel", ctypes.c_int64), ("dy_image", ctypes.c_int64),
+                ("dy_pixel", ctypes.c_int64)]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("x_type", ctypes.c_int32), ("out_type", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("x_row", ctypes.c_int64), ("out_row", ctypes.c_int64)]
 
 
 class PatdnnError(RuntimeError):
@@ -124,6 +143,18 @@ def lib() -> ctypes.CDLL:
         L.patdnn_selftest.argtypes = []
         L.patdnn_destroy.argtypes = [vp]
         L.patdnn_destroy.restype = None
+        i64, size = ctypes.c_int64, ctypes.c_size_t
+        L.patdnn_channels_last.argtypes = [vp, i32, i32, i32, i32, vp, i32, i64, i64, vp]
+        L.patdnn_channels_first.argtypes = [vp, i32, i64, i64, i32, i32, i32, vp, i32, vp]
+        L.patdnn_group_norm.argtypes = [ctypes.POINTER(NormDesc), vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.patdnn_group_norm_backward.argtypes = [ctypes.POINTER(NormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.patdnn_group_norm_workspace_floats.argtypes = [ctypes.POINTER(NormDesc), i32]
+        L.patdnn_group_norm_workspace_floats.restype = size
+        L.patdnn_mxfp4_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp]
+        L.patdnn_mxfp4_dequantize.argtypes = [vp, vp, i32, i32, vp, i32, i64, vp]
+        L.patdnn_mxfp4_linear.argtypes = [ctypes.POINTER(LinearDesc), vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.patdnn_mxfp4_linear_workspace_bytes.argtypes = [ctypes.POINTER(LinearDesc)]
+        L.patdnn_mxfp4_linear_workspace_bytes.restype = size
         L.patdnn_status_string.argtypes = [i32]
         L.patdnn_status_string.restype = ctypes.c_char_p
         L.patdnn_last_error.argtypes = []
@@ -452,6 +483,252 @@ def patdnn_selftest() -> None:
 def patdnn_destroy(handle: Optional[int]) -> None:
     if handle:
         lib().patdnn_destroy(handle)
+
+
+# ---------------------------------------------------------------------------
+# what stands between and behind the convolutions: order of channels, group norm, MXFP4
+# ---------------------------------------------------------------------------
+
+_types = None
+
+
+def _type(dtype) -> int:
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: PATDNN_F32, torch.float16: PATDNN_F16, torch.bfloat16: PATDNN_BF16}
+    try:
+        return _types[dtype]
+    except KeyError:
+        raise ValueError(f"float32, float16 or bfloat16 expected, not {dtype}") from None
+
+
+def _act(act: str) -> int:
+    try:
+        return ACTIVATIONS[act]
+    except KeyError:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}") from None
+
+
+def _new(shape, dtype, like, stream):
+    """A tensor that the call's stream owns: what is allocated while another one is current may not be in use there
+    any more before it is here, nor free here before it is there."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream(like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _float_vector(t, count: int, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.float32 or t.numel() != count:
+        raise ValueError(f"{name} must be float32 with {count} elements")
+    return _devptr(t)
+
+
+def _channels_last_layout(t, name: str):
+    """[n, ..., c] -> (n, pixels, c, image stride, pixel stride)."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    shape, strides = t.shape, t.stride()
+    if len(shape) < 3:
+        raise ValueError(f"{name} must be [n, ..., channels]")
+    c = shape[-1]
+    if c > 1 and strides[-1] != 1 and t.numel():
+        raise ValueError(f"the channels of {name} must be adjacent")
+    pixel, pixels = strides[-2], shape[-2]
+    for i in range(len(shape) - 3, 0, -1):
+        if pixels == 1:
+            pixel = strides[i]
+        elif shape[i] > 1 and strides[i] != pixel * pixels and t.numel():
+            raise ValueError(f"the pixels of {name} must be evenly spaced")
+        pixels *= shape[i]
+    return shape[0], pixels, c, strides[0], pixel
+
+
+def patdnn_channels_last(x, out=None, *, dtype=None, stream=None):
+    """x [n, c, h, w], dense -> [n, h, w, c] of type ``dtype`` (x's if None); ``out`` may be a slice of the channels of a wider tensor."""
+    if x.dim() != 4:
+        raise ValueError("input must be a 4-d tensor")
+    n, c, h, w = x.shape
+    if out is None:
+        out = _new((n, h, w, c), dtype or x.dtype, x, stream)
+    elif tuple(out.shape) != (n, h, w, c) or (dtype and out.dtype != dtype):
+        raise ValueError(f"output must be {(n, h, w, c)}, of type dtype if that is given")
+    _, _, _, image, pixel = _channels_last_layout(out, "output")
+    _check(lib().patdnn_channels_last(_devptr(x), _type(x.dtype), n, c, h * w, out.data_ptr(), _type(out.dtype), image, pixel,
+                                      _stream_ptr(stream)))
+    return out
+
+
+def patdnn_channels_first(x, out=None, *, dtype=None, stream=None):
+    """x [n, h, w, c], maybe a slice of the channels of a wider tensor -> [n, c, h, w], dense, of type ``dtype`` (x's if None)."""
+    if x.dim() != 4:
+        raise ValueError("input must be a 4-d tensor")
+    n, h, w, c = x.shape
+    _, _, _, image, pixel = _channels_last_layout(x, "input")
+    if out is None:
+        out = _new((n, c, h, w), dtype or x.dtype, x, stream)
+    elif tuple(out.shape) != (n, c, h, w) or (dtype and out.dtype != dtype):
+        raise ValueError(f"output must be {(n, c, h, w)}, of type dtype if that is given")
+    _check(lib().patdnn_channels_first(x.data_ptr(), _type(x.dtype), image, pixel, n, c, h * w, _devptr(out), _type(out.dtype),
+                                       _stream_ptr(stream)))
+    return out
+
+
+def _norm_workspace(desc, backward: int, workspace, like, stream):
+    import torch
+    floats = lib().patdnn_group_norm_workspace_floats(ctypes.byref(desc), backward)
+    if workspace is None:
+        workspace = _new((floats,), torch.float32, like, stream)
+    elif workspace.dtype != torch.float32:
+        raise ValueError("workspace must be a float32 tensor")
+    return workspace
+
+
+def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e-5, act="none", mean=None, rstd=None, workspace=None,
+                      stream=None):
+    """x [n, ..., c] channels last -> (act(group norm) like x, mean, rstd float32 [n, groups]).  gamma, beta: float32 [c] or None.
+    x and ``out`` may be slices of the channels of wider tensors."""
+    import torch
+    n, pixels, c, x_image, x_pixel = _channels_last_layout(x, "x")
+    if out is None:
+        out = _new(tuple(x.shape), x.dtype, x, stream)
+    elif out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("output must have the shape and type of x")
+    _, _, _, y_image, y_pixel = _channels_last_layout(out, "output")
+    if mean is None:
+        mean = _new((n, groups), torch.float32, x, stream)
+    if rstd is None:
+        rstd = _new((n, groups), torch.float32, x, stream)
+    desc = NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), eps, x_image, x_pixel, y_image, y_pixel, 0, 0)
+    workspace = _norm_workspace(desc, 0, workspace, x, stream)
+    _check(lib().patdnn_group_norm(ctypes.byref(desc), x.data_ptr(), _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"),
+                                   out.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
+                                   _devptr(workspace), workspace.numel(), _stream_ptr(stream)))
+    return out, mean, rstd
+
+
+def patdnn_group_norm_backward(dy, x, mean, rstd, groups: int, gamma=None, beta=None, out=None, *, act="none", dgamma=None, dbeta=None,
+                               workspace=None, stream=None):
+    """Gradients of patdnn_group_norm: (dx like x, dgamma, dbeta float32 [c]) from dy, x and the forward call's mean and rstd."""
+    import torch
+    n, pixels, c, x_image, x_pixel = _channels_last_layout(x, "x")
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError("dy must have the shape and type of x")
+    _, _, _, dy_image, dy_pixel = _channels_last_layout(dy, "dy")
+    if out is None:
+        out = _new(tuple(x.shape), x.dtype, x, stream)
+    elif out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("output must have the shape and type of x")
+    _, _, _, y_image, y_pixel = _channels_last_layout(out, "output")
+    if dgamma is None:
+        dgamma = _new((c,), torch.float32, x, stream)
+    if dbeta is None:
+        dbeta = _new((c,), torch.float32, x, stream)
+    desc = NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), 0.0, x_image, x_pixel, y_image, y_pixel, dy_image, dy_pixel)
+    workspace = _norm_workspace(desc, 1, workspace, x, stream)
+    _check(lib().patdnn_group_norm_backward(
+        ctypes.byref(desc), dy.data_ptr(), x.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
+        _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"), out.data_ptr(), _float_vector(dgamma, c, "dgamma"),
+        _float_vector(dbeta, c, "dbeta"), _devptr(workspace), workspace.numel(), _stream_ptr(stream)))
+    return out, dgamma, dbeta
+
+
+def _rows(t, name: str) -> int:
+    """Elements between the rows of a 2-d tensor whose rows' values are adjacent."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-d tensor")
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    row, step = t.stride()
+    if step != 1 and t.shape[1] > 1 and t.numel():
+        raise ValueError(f"the values of a row of {name} must be adjacent")
+    return row
+
+
+def _codes(codes, scales, rows: int, cols: int):
+    import torch
+    pieces = -(-cols // 128)
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.shape != (rows, pieces * 64) or scales.shape != (rows, pieces * 4):
+        raise ValueError(f"codes and scales must be uint8 {(rows, pieces * 64)} and {(rows, pieces * 4)}")
+    return _devptr(codes), _devptr(scales)
+
+
+def patdnn_mxfp4_quantize(x, codes=None, scales=None, *, stream=None):
+    """x [rows, cols] -> (codes uint8 [rows, ceil(cols/128)*64], scales uint8 [rows, ceil(cols/128)*4])."""
+    import torch
+    row = _rows(x, "x")
+    rows, cols = x.shape
+    pieces = -(-cols // 128)
+    if codes is None:
+        codes = _new((rows, pieces * 64), torch.uint8, x, stream)
+    if scales is None:
+        scales = _new((rows, pieces * 4), torch.uint8, x, stream)
+    cp, sp = _codes(codes, scales, rows, cols)
+    _check(lib().patdnn_mxfp4_quantize(x.data_ptr(), _type(x.dtype), rows, cols, row, cp, sp, _stream_ptr(stream)))
+    return codes, scales
+
+
+def patdnn_mxfp4_dequantize(codes, scales, cols: int, out=None, *, dtype=None, stream=None):
+    """The values [rows, cols] that codes and scales stand for, float32 unless ``out`` or ``dtype`` says otherwise."""
+    import torch
+    rows = codes.shape[0]
+    cp, sp = _codes(codes, scales, rows, cols)
+    if out is None:
+        out = _new((rows, cols), dtype or torch.float32, codes, stream)
+    elif tuple(out.shape) != (rows, cols) or (dtype and out.dtype != dtype):
+        raise ValueError(f"output must be {(rows, cols)}, of type dtype if that is given")
+    row = _rows(out, "output")
+    _check(lib().patdnn_mxfp4_dequantize(cp, sp, rows, cols, out.data_ptr(), _type(out.dtype), row, _stream_ptr(stream)))
+    return out
+
+
+def patdnn_mxfp4_linear(x, w, w_scales, bias=None, out=None, *, x_scales=None, act="none", dtype=None, workspace=None, stream=None):
+    """x [rows, in] times MXFP4 weights [out, in], plus bias (float32 [out]), activated.  x is float32 / float16 / bfloat16, or the codes
+    of patdnn_mxfp4_quantize with ``x_scales``.  The result's type: ``out``'s, ``dtype``, or x's (float32 for codes)."""
+    import torch
+    row = _rows(x, "x")
+    features = w.shape[0]
+    if x_scales is None:
+        rows, cols = x.shape
+        kind, sp = _type(x.dtype), None
+    else:
+        rows, cols = x.shape[0], x.shape[1] * 2
+        kind, row = PATDNN_MXFP4, 0
+        _, sp = _codes(x, x_scales, rows, cols)
+    wp, wsp = _codes(w, w_scales, features, cols)
+    if out is None:
+        out = _new((rows, features), dtype or (x.dtype if x_scales is None else torch.float32), x, stream)
+    elif tuple(out.shape) != (rows, features) or (dtype and out.dtype != dtype):
+        raise ValueError(f"output must be {(rows, features)}, of type dtype if that is given")
+    desc = LinearDesc(rows, cols, features, kind, _type(out.dtype), _act(act), row, _rows(out, "output"))
+    needs = lib().patdnn_mxfp4_linear_workspace_bytes(ctypes.byref(desc))
+    if needs and workspace is None:
+        workspace = _new((needs,), torch.uint8, x, stream)
+    _check(lib().patdnn_mxfp4_linear(ctypes.byref(desc), x.data_ptr(), sp, wp, wsp, _float_vector(bias, features, "bias"), out.data_ptr(),
+                                     _devptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                     _stream_ptr(stream)))
+    return out
+
+
+def patdnn_mxfp4_linear_workspace_bytes(rows: int, in_features: int, out_features: int, *, x_type: int, out_type: int) -> int:
+    """Bytes of workspace for a call of patdnn_mxfp4_linear with dense rows."""
+    desc = LinearDesc(rows, in_features, out_features, x_type, out_type, 0, in_features, out_features)
+    return int(lib().patdnn_mxfp4_linear_workspace_bytes(ctypes.byref(desc)))
+
+
+def patdnn_group_norm_workspace_floats(n: int, pixels: int, channels: int, groups: int, *, type: int = PATDNN_F32,
+                                       backward: bool = False) -> int:
+    """Floats of workspace for a call of patdnn_group_norm, or of its backward pass, on dense tensors."""
+    image = pixels * channels
+    desc = NormDesc(n, pixels, channels, groups, type, 0, 0.0, image, channels, image, channels, image, channels)
+    return int(lib().patdnn_group_norm_workspace_floats(ctypes.byref(desc), int(bool(backward))))
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,137 @@
+"""What the operators around the convolutions refuse, before anything reaches a device: status, and a text that names the reason."""
+
+import ctypes
+
+import pytest
+
+from paper_2001_00138_amd import binding as B
+
+L = B.lib
+P = 1 << 20                   # stands for device addresses that no call gets as far as reading
+Q, R, S, T = P << 8, P << 9, P << 10, P << 11
+
+
+def _refused(status, word, call, *args):
+    assert call(*args) == status
+    assert word in L().patdnn_last_error().decode()
+
+
+def test_reorder():
+    last, first = L().patdnn_channels_last, L().patdnn_channels_first
+    good = [P, 0, 2, 8, 9, Q, 1, 72, 8, None]
+    for at, value, word in [(1, 3, "type"), (6, -1, "type"), (2, -1, "n must"), (3, 0, "positive"), (4, 0, "positive"), (7, 71, "strides"), (8, 7, "strides"),
+                            (7, -1, "strides"), (0, None, "NULL"), (5, None, "NULL"), (0, P + 2, "aligned"), (5, Q + 1, "aligned"), (5, P + 64, "overlap")]:
+        _refused(B.PATDNN_EINVAL, word, last, *[value if i == at else v for i, v in enumerate(good)])
+    good = [P, 0, 72, 8, 2, 8, 9, Q, 1, None]
+    for at, value, word in [(1, 3, "type"), (8, 7, "type"), (2, -1, "strides"), (3, -8, "strides"), (4, -1, "n must"), (5, 0, "positive"),
+                            (6, -4, "positive"), (0, None, "NULL"), (7, P, "overlap")]:
+        _refused(B.PATDNN_EINVAL, word, first, *[value if i == at else v for i, v in enumerate(good)])
+    _refused(B.PATDNN_EUNSUPPORTED, "large", first, P, 0, 1 << 60, 8, 2, 8, 9, Q, 1, None)
+    _refused(B.PATDNN_EUNSUPPORTED, "large", first, P, 0, 0, 0, 2 ** 31 - 1, 2 ** 20, 2 ** 20, Q, 1, None)
+    assert last(P, 0, 0, 8, 9, None, 1, 72, 8, None) == B.PATDNN_OK                   # no images
+
+
+def _norm(**change):
+    d = dict(n=2, pixels=9, channels=8, groups=4, type=0, act=0, eps=1e-5, x_image=72, x_pixel=8, y_image=72, y_pixel=8, dy_image=72, dy_pixel=8)
+    d.update(change)
+    return ctypes.byref(B.NormDesc(*(d[k] for k, _ in B.NormDesc._fields_)))
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(n=-1), "n must"), (dict(pixels=0), "positive"), (dict(channels=0), "positive"), (dict(groups=0), "positive"), (dict(groups=3), "divide"),
+    (dict(type=3), "type"), (dict(act=3), "activation"), (dict(act=-1), "activation"), (dict(x_image=-1), "strides"), (dict(x_pixel=-1), "strides"),
+    (dict(y_pixel=7), "overlap"), (dict(y_image=71), "overlap"), (dict(y_image=-1), "overlap")])
+def test_norm_description(change, word):
+    big = 1 << 20
+    _refused(B.PATDNN_EINVAL, word, L().patdnn_group_norm, _norm(**change), P, None, None, Q, None, None, R, big, None)
+    _refused(B.PATDNN_EINVAL, word, L().patdnn_group_norm_backward, _norm(**change), S, P, T, T, None, None, Q, None, None, R, big, None)
+    assert L().patdnn_group_norm_workspace_floats(_norm(**change), 0) == 0
+
+
+def test_norm_arguments():
+    f, b, big = L().patdnn_group_norm, L().patdnn_group_norm_backward, 1 << 20
+    needs = L().patdnn_group_norm_workspace_floats(_norm(), 0)
+    assert needs > 0
+    for eps in (-1.0, float("nan"), float("inf")):
+        _refused(B.PATDNN_EINVAL, "eps", f, _norm(eps=eps), P, None, None, Q, None, None, R, big, None)
+    good = [_norm(), P, None, None, Q, None, None, R, big, None]
+    for at, value, word in [(0, None, "desc"), (1, None, "NULL"), (4, None, "NULL"), (1, P + 2, "aligned"), (2, P + 1, "aligned"), (5, T + 2, "aligned"),
+                            (4, P + 8, "overlaps input"), (7, None, "workspace"), (8, needs - 1, "workspace"), (7, P, "workspace"), (7, Q, "workspace")]:
+        _refused(B.PATDNN_EINVAL, word, f, *[value if i == at else v for i, v in enumerate(good)])
+    good = [_norm(), S, P, T, T + 64, None, None, Q, None, None, R, big, None]
+    for at, value, word in [(1, None, "NULL"), (2, None, "NULL"), (3, None, "NULL"), (4, None, "NULL"), (7, None, "NULL"), (7, P, "overlaps input"),
+                            (7, S + 4, "overlaps input"), (8, T + 1, "aligned"), (10, None, "workspace"), (11, 1, "workspace"), (10, S, "workspace")]:
+        _refused(B.PATDNN_EINVAL, word, b, *[value if i == at else v for i, v in enumerate(good)])
+    _refused(B.PATDNN_EINVAL, "strides", b, _norm(dy_pixel=-1), S, P, T, T, None, None, Q, None, None, R, big, None)
+    _refused(B.PATDNN_EUNSUPPORTED, "large", f, _norm(n=2 ** 31 - 1, y_image=1 << 40), P, None, None, Q, None, None, R, big, None)
+    _refused(B.PATDNN_EUNSUPPORTED, "large", f, _norm(x_image=1 << 61), P, None, None, Q, None, None, R, big, None)
+    assert f(_norm(n=0), None, None, None, None, None, None, None, 0, None) == B.PATDNN_OK
+
+
+def test_quantise():
+    q, d = L().patdnn_mxfp4_quantize, L().patdnn_mxfp4_dequantize
+    good = [P, 0, 3, 40, 40, Q, R, None]
+    for at, value, word in [(1, 3, "type"), (2, -1, "rows"), (3, 0, "positive"), (4, -1, "strides"), (0, None, "NULL"), (5, None, "NULL"), (6, None, "NULL"),
+                            (5, Q + 8, "aligned"), (6, R + 2, "aligned"), (0, P + 2, "aligned"), (5, P + 16, "overlap"), (6, P + 4, "overlap"), (6, Q, "overlap")]:
+        _refused(B.PATDNN_EINVAL, word, q, *[value if i == at else v for i, v in enumerate(good)])
+    good = [Q, R, 3, 40, P, 0, 40, None]
+    for at, value, word in [(5, 3, "type"), (6, 39, "overlap"), (4, None, "NULL"), (0, P + 16, "overlap"), (1, P + 4, "overlap")]:
+        _refused(B.PATDNN_EINVAL, word, d, *[value if i == at else v for i, v in enumerate(good)])
+    _refused(B.PATDNN_EUNSUPPORTED, "large", q, P, 0, 3, 2 ** 31 - 1, 1, Q, R, None)
+    assert q(None, 0, 0, 40, 40, None, None, None) == B.PATDNN_OK
+
+
+def _linear(**change):
+    d = dict(rows=20, in_features=40, out_features=7, x_type=0, out_type=0, act=0, x_row=40, out_row=7)
+    d.update(change)
+    return ctypes.byref(B.LinearDesc(*(d[k] for k, _ in B.LinearDesc._fields_)))
+
+
+def test_linear():
+    f, big = L().patdnn_mxfp4_linear, 1 << 20
+    good = [_linear(), P, None, Q, Q + 4096, None, R, S, big, None]
+    for change, word in [(dict(rows=-1), "rows"), (dict(in_features=0), "positive"), (dict(out_features=-3), "positive"), (dict(x_type=4), "type"),
+                         (dict(out_type=3), "type"), (dict(act=9), "activation"), (dict(x_row=-1), "strides"), (dict(out_row=6), "overlap")]:
+        _refused(B.PATDNN_EINVAL, word, f, _linear(**change), *good[1:])
+        assert L().patdnn_mxfp4_linear_workspace_bytes(_linear(**change)) == 0
+    needs = L().patdnn_mxfp4_linear_workspace_bytes(_linear())
+    assert needs > 0
+    for at, value, word in [(0, None, "desc"), (1, None, "NULL"), (6, None, "NULL"), (3, None, "NULL"), (4, None, "NULL"), (3, Q + 4, "aligned"),
+                            (4, Q + 4097, "aligned"), (1, P + 1, "aligned"), (5, P + 2, "aligned"), (6, P, "overlaps input"), (6, Q + 16, "overlaps input"),
+                            (6, Q + 4096, "overlaps input"), (5, R, "overlaps input"), (7, None, "workspace"), (8, needs - 1, "workspace"),
+                            (7, S + 4, "workspace"), (7, R, "workspace"), (7, Q, "workspace")]:
+        _refused(B.PATDNN_EINVAL, word, f, *[value if i == at else v for i, v in enumerate(good)])
+    _refused(B.PATDNN_EINVAL, "scales", f, _linear(x_type=3), P, None, *good[3:])
+    _refused(B.PATDNN_EINVAL, "aligned", f, _linear(x_type=3), P + 4, T, *good[3:])
+    _refused(B.PATDNN_EUNSUPPORTED, "large", f, _linear(rows=2 ** 31 - 1, out_features=2 ** 31 - 1, out_row=2 ** 31), *good[1:])
+    assert f(_linear(rows=0), None, None, None, None, None, None, None, 0, None) == B.PATDNN_OK
+
+
+def test_the_binding():
+    import torch
+    x = torch.zeros(2, 4, 4, 8)
+    with pytest.raises(ValueError, match="device tensor"):
+        B.patdnn_group_norm(x, 2)
+    with pytest.raises(ValueError, match="device tensor"):
+        B.patdnn_mxfp4_quantize(x.view(32, 8))
+    with pytest.raises(ValueError, match="4-d"):
+        B.patdnn_channels_last(x[0])
+    with pytest.raises(ValueError, match="act"):
+        B._act("gelu")
+    with pytest.raises(ValueError, match="float32"):
+        B._type(torch.float64)
+    class Fake:                                        # a layout without memory behind it
+        is_cuda = True
+        def __init__(self, shape, strides):
+            self.shape, self._strides = shape, strides
+        def stride(self):
+            return self._strides
+        def numel(self):
+            return 1
+    assert B._channels_last_layout(Fake((2, 3, 4, 5), (100, 20, 5, 1)), "x") == (2, 12, 5, 100, 5)
+    assert B._channels_last_layout(Fake((2, 3, 1, 5), (100, 20, 77, 1)), "x") == (2, 3, 5, 100, 20)
+    assert B._channels_last_layout(Fake((2, 1, 4, 5), (100, 99, 6, 1)), "x") == (2, 4, 5, 100, 6)
+    assert B._channels_last_layout(Fake((2, 3, 4, 5), (0, 0, 0, 1)), "x") == (2, 12, 5, 0, 0)
+    for layout, word in [(Fake((2, 3, 4, 5), (100, 21, 5, 1)), "evenly"), (Fake((2, 3, 4, 5), (60, 4, 1, 12)), "adjacent"), (Fake((2, 5), (5, 1)), "n, ...")]:
+        with pytest.raises(ValueError, match=word):
+            B._channels_last_layout(layout, "x")

@@ -9,9 +9,7 @@
 // and the workgroup's wavefronts add their sums up in LDS, in the order of the ranges.
 #include <type_traits>
 
-#include "kernels.hpp"
-#include "mxfp4.hpp"
-#include "operators.hpp"
+#include "linear.hpp"
 
 namespace patdnn {
 
@@ -26,17 +24,6 @@ struct Args {
     bool whole_runs;                                     // rows of x in runs of 16 bytes
     FastDiv by_n;
 };
-
-__device__ __forceinline__ void store_as(void* out, long long at, int type, float v)
-{
-    if (type == kF32) static_cast<float*>(out)[at] = v;
-    else if (type == kF16) static_cast<_Float16*>(out)[at] = static_cast<_Float16>(v);
-    else static_cast<__bf16*>(out)[at] = static_cast<__bf16>(v);
-}
-__device__ __forceinline__ float activate_as(float z, int act)
-{
-    return act == kActRelu ? activate<kActRelu>(z) : act == kActSilu ? activate<kActSilu>(z) : z;
-}
 
 // This lane's block of 32 values of row m: codes and scale byte.
 template <class X>
@@ -140,30 +127,49 @@ bool linear_fits(const LinearShape& s)
            mxfp4_fits(Mxfp4Shape{s.rows, s.in, kF32, s.in});
 }
 
-size_t linear_workspace_bytes(const LinearShape& s)
+namespace {
+
+// The workspace: codes and scales of x where it is quantised beforehand, then the slices' sums.
+struct Room {
+    bool quantised_here;
+    TilePlan plan;
+    size_t scales_at, sums_at, bytes;
+};
+Room room_of(const LinearShape& s)
 {
-    if (s.x_type == kMxfp4 || s.rows <= kDirectRows) return 0;
-    return (size_t)s.rows * (size_t)mxfp4_pieces(s.in) * 68;
+    Room r{};
+    r.quantised_here = s.x_type != kMxfp4 && s.rows > kDirectRows;
+    r.plan = tile_plan(s);
+    const size_t blocks = r.quantised_here ? (size_t)s.rows * (size_t)mxfp4_pieces(s.in) * 4 : 0;
+    r.scales_at = blocks * 16;
+    r.sums_at = (r.scales_at + blocks + 15) / 16 * 16;
+    r.bytes = r.sums_at + tile_workspace_bytes(s, r.plan);
+    return r;
 }
+
+}  // namespace
+
+size_t linear_workspace_bytes(const LinearShape& s) { return room_of(s).bytes; }
 
 hipError_t launch_linear(const LinearShape& s, const void* x, const uint8_t* x_scales, const uint8_t* w, const uint8_t* w_scales, const float* bias,
                          void* out, void* workspace, hipStream_t stream)
 {
-    if (s.x_type != kMxfp4 && s.rows <= kDirectRows) {
+    const Room room = room_of(s);
+    uint8_t* work = static_cast<uint8_t*>(workspace);
+    if (s.x_type != kMxfp4 && !room.quantised_here) {
         hipError_t e = hipSuccess;
         with_type(s.x_type, [&](auto t) { e = launch_direct<decltype(t), 1, 1>(s, x, nullptr, w, w_scales, bias, out, stream); });
         return e;
     }
-    if (s.x_type != kMxfp4) {
-        uint8_t* codes = static_cast<uint8_t*>(workspace);
-        uint8_t* scales = codes + (size_t)s.rows * (size_t)mxfp4_pieces(s.in) * 64;
-        const hipError_t e = launch_mxfp4_quantize(Mxfp4Shape{s.rows, s.in, s.x_type, s.x_row}, x, codes, scales, stream);
+    if (room.quantised_here) {
+        const hipError_t e = launch_mxfp4_quantize(Mxfp4Shape{s.rows, s.in, s.x_type, s.x_row}, x, work, work + room.scales_at, stream);
         if (e != hipSuccess) return e;
-        x = codes;
-        x_scales = scales;
+        x = work;
+        x_scales = work + room.scales_at;
     }
-    return s.rows <= 16 ? launch_direct<Codes, 1, 1>(s, x, x_scales, w, w_scales, bias, out, stream)
-                        : launch_direct<Codes, 4, 4>(s, x, x_scales, w, w_scales, bias, out, stream);
+    if (room.plan.shape >= 0)
+        return launch_tiles(s, room.plan, x, x_scales, w, w_scales, bias, out, reinterpret_cast<float*>(work + room.sums_at), stream);
+    return launch_direct<Codes, 1, 1>(s, x, x_scales, w, w_scales, bias, out, stream);
 }
 
 }  // namespace patdnn

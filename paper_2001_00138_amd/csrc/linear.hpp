@@ -1,0 +1,31 @@
+// What the two files of the linear layer's kernels share.
+#pragma once
+
+#include "kernels.hpp"
+#include "mxfp4.hpp"
+#include "operators.hpp"
+
+namespace patdnn {
+
+__device__ __forceinline__ void store_as(void* out, long long at, int type, float v)
+{
+    if (type == kF32) static_cast<float*>(out)[at] = v;
+    else if (type == kF16) static_cast<_Float16*>(out)[at] = static_cast<_Float16>(v);
+    else static_cast<__bf16*>(out)[at] = static_cast<__bf16>(v);
+}
+__device__ __forceinline__ float activate_as(float z, int act)
+{
+    return act == kActRelu ? activate<kActRelu>(z) : act == kActSilu ? activate<kActSilu>(z) : z;
+}
+
+// The tiled kernel (kernel_linear_tiles.hip), codes times codes.  Which shape it takes, and along how many slices of k.
+struct TilePlan {
+    int shape = -1;                                      // -1: not this kernel
+    int slices = 1;
+};
+TilePlan tile_plan(const LinearShape& s);
+size_t tile_workspace_bytes(const LinearShape& s, const TilePlan& p);
+hipError_t launch_tiles(const LinearShape& s, const TilePlan& p, const void* x, const uint8_t* x_scales, const uint8_t* w, const uint8_t* w_scales,
+                        const float* bias, void* out, float* partial, hipStream_t stream);
+
+}  // namespace patdnn

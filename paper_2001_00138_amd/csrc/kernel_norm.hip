@@ -5,7 +5,8 @@
 //   dbeta = sum of dz and dgamma = sum of dz xh over images and pixels, per channel;
 //   dx = r (gamma dz - (A + xh B) / M), A and B the sums of gamma dz and gamma dz xh over the group.
 //
-// Both read what they normalise twice, once for the sums and once to apply them: two launches.  A workgroup takes a
+// Where a workgroup can hold the pixels of some whole groups in its registers it reads them once and needs no second launch (the
+// "held" kernels below).  Otherwise what is normalised is read twice, once for the sums and once to apply them: a workgroup takes a
 // slab of pixels and a chunk of channels that holds whole groups (or a part of one group, if that has more than
 // kChunk channels); a lane keeps V adjacent channels and walks the slab's pixels, so that lanes read whole cache
 // lines and channels need no shuffling.  Slabs leave their sums in the workspace; the second launch adds them up
@@ -13,8 +14,8 @@
 //
 // Statistics are fp32.  Every lane runs Welford's update (mean and sum of squared distances from it), and partial results
 // are joined by Chan's formula: neither subtracts large squares from each other, so values far from zero keep
-// their variance.  z is rounded after each of its four operations, forward and backward alike, so that the two agree about
-// the sign that decides ReLU's gradient.
+// their variance.  With ReLU z is rounded after each of its four operations, forward and backward alike, so
+// that the two agree about the sign that decides its gradient.
 #include "kernels.hpp"
 #include "operators.hpp"
 
@@ -34,6 +35,7 @@ struct Geometry {
     int slab, slabs;                 // pixels of a slab, slabs of an image
     int tx, ty;                      // lanes side by side over channels, and over pixels
     int join;                        // lanes that join the sums of one group (a power of two up to 64)
+    int runs, full, last_runs, last_full;        // pixels that the first `full` rows of lanes have, the others one less; of the last slab
     float inv_m;                     // 1 / (pixels * cpg)
     FastDiv by_slabs, by_chunks, by_tx, by_cpg;
 };
@@ -168,8 +170,8 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(Geometry G, const 
         float mean, m2;
         join_stats(per * G.ty, lane, G.join, [&](int i, float& ni, float& mi, float& si) {
             const int row = G.per_group == 1 ? (int)fast_div((uint32_t)i, by_per) : i / per;
-            const int at = row * pitch + g * per + (i - row * per), left = w.p1 - w.p0 - row;
-            ni = left > 0 ? (float)((left + G.ty - 1) / G.ty) : 0.0f;
+            const int at = row * pitch + g * per + (i - row * per), pixels = w.p1 - w.p0;
+            ni = (float)(pixels == G.slab ? G.runs - (row >= G.full) : G.last_runs - (row >= G.last_full));
             mi = s_mean[at];
             si = s_m2[at];
         }, mean, m2);
@@ -193,8 +195,29 @@ __device__ __forceinline__ float part_count(const Geometry& G, int part)
 }
 
 // xh and z of the comment at the top, rounded after each operation.
-__device__ __forceinline__ float normalised(float x, float mean, float rstd) { return __fmul_rn(__fsub_rn(x, mean), rstd); }
-__device__ __forceinline__ float affine(float xh, float gamma, float beta) { return __fadd_rn(__fmul_rn(xh, gamma), beta); }
+__device__ __forceinline__ float centred(float x, float mean)
+{
+#pragma clang fp contract(off)
+    return x - mean;
+}
+__device__ __forceinline__ float affine(float d, float rstd, float gamma, float beta)
+{
+#pragma clang fp contract(off)
+    return d * rstd * gamma + beta;
+}
+
+// Without ReLU nothing jumps where z is 0, and z = x a + b takes one operation instead of four: a = rstd gamma and b = beta - mean a go into
+// gamma's and beta's places.
+__device__ __forceinline__ void straight(float mean, float rstd, float& gamma, float& beta)
+{
+    gamma *= rstd;
+    beta = fmaf(-mean, gamma, beta);
+}
+template <int ACT>
+__device__ __forceinline__ float apply_one(float x, float mean, float rstd, float gamma, float beta)
+{
+    return activate<ACT>(ACT == kActRelu ? affine(centred(x, mean), rstd, gamma, beta) : fmaf(x, gamma, beta));
+}
 
 template <class T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Geometry G, const T* __restrict__ x, const float* __restrict__ gamma,
@@ -237,34 +260,274 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Geometry G, const 
         rstd[i] = s_rstd[g];
         ga[i] = gamma ? gamma[w.c0 + c + i] : 1.0f;
         be[i] = beta ? beta[w.c0 + c + i] : 0.0f;
+        if (ACT != kActRelu) straight(mean[i], rstd[i], ga[i], be[i]);
     }
     T* to = y + w.n * G.s.y_image + first * G.s.y_pixel + w.c0 + c;
     walk<T, V>(x + w.n * G.s.x_image + first * G.s.x_pixel + w.c0 + c, G.ty * G.s.x_pixel, (w.p1 - first + G.ty - 1) / G.ty, [&](const float (&v)[V]) {
         Pack<T, V> r;
 #pragma unroll
-        for (int i = 0; i < V; ++i) r.v[i] = from_float<T>(activate<ACT>(affine(normalised(v[i], mean[i], rstd[i]), ga[i], be[i])));
+        for (int i = 0; i < V; ++i) r.v[i] = from_float<T>(apply_one<ACT>(v[i], mean[i], rstd[i], ga[i], be[i]));
         store_pack<T, V>(to, r);
         to += G.ty * G.s.y_pixel;
     });
 }
 
+// ---- held in registers ----
+
+// A workgroup holds all pixels of `chunk` channels (whole groups) of one image: lane (ty, tx) has channels tx V ... of pixels ty, ty + G.ty, ...
+struct Held {
+    NormShape s;
+    int cpg, chunk, chunks, tx, ty, join;
+    int span, entries;                                   // channels of a lane that are joined before others see them; what a row of lanes adds to a group
+    int folded, lanes;                                   // a group's lanes in a row are a power of two (`lanes`), and the rows too: sums fold by exchange
+    int runs, full;                                      // runs that the first `full` rows of lanes have, the others one less
+    float inv_m;
+    FastDiv by_chunks, by_tx, by_cpg, by_entries;
+};
+
+// Most runs that a lane holds: 64 registers of them (32 of one or two bytes).
+template <class T, int V>
+constexpr int held_runs() { return V * sizeof(T) >= 16 ? 16 : 32; }
+
+__device__ __forceinline__ uint32_t held_block(uint32_t total)
+{
+    // neighbouring chunks share cache lines: each XCD (workgroups go to the eight in turn) takes a run of them
+    const uint32_t xcd = blockIdx.x & 7, q = total >> 3, rest = total & 7;
+    return xcd * q + min(xcd, rest) + (blockIdx.x >> 3);
+}
+
+// Registers that hold a run.  used(sum) keeps the compiler from holding the values that it widened the run to as well, once `sum`
+// has them.
+template <class T, int V>
+struct Kept {
+    static constexpr int kWords = V * sizeof(T) >= 4 ? V * (int)sizeof(T) / 4 : 1;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (V * sizeof(T) >= 4) {
+            const Pack<uint32_t, kWords> a = load_pack<uint32_t, kWords>(reinterpret_cast<const uint32_t*>(p));
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = a.v[i];
+        } else {
+            w[0] = *reinterpret_cast<const unsigned short*>(p);
+        }
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return to_float(__builtin_bit_cast(T, (unsigned short)(i & 1 ? w[i / 2] >> 16 : w[i / 2])));
+    }
+    template <int N>
+    __device__ __forceinline__ void used(float (&sum)[N])
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+#pragma unroll
+            for (int j = 0; j < N; j += 2) {
+                if (j + 1 < N) asm volatile("" : "+v"(w[i]), "+v"(sum[j]), "+v"(sum[j + 1 < N ? j + 1 : j]));
+                else asm volatile("" : "+v"(w[i]), "+v"(sum[j]));
+            }
+    }
+};
+
+// Sum over a workgroup of what its lanes have for their group: over the lanes of a wavefront by exchange, over the wavefronts
+// through s_part.
+__device__ __forceinline__ float fold(const Held& G, float v, int c, int groups, int wave, int waves, float* s_part)
+{
+    for (int d = 1; d < G.lanes; d *= 2) v += __shfl_xor(v, d, 64);
+    for (int d = G.tx; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
+    const int g = c < groups * G.cpg ? (int)fast_div((uint32_t)c, G.by_cpg) : 0;
+    if (((int)threadIdx.x & 63) < G.tx && c < groups * G.cpg) s_part[wave * groups + g] = v;       // the wavefront's first row of lanes
+    __syncthreads();
+    v = 0.0f;
+    for (int k = 0; k < waves; ++k) v += s_part[k * groups + g];
+    return v;
+}
+
+// ONE: the V channels of a lane are of one group.
+template <class T, int V, int R, bool ONE>
+__global__ __launch_bounds__(1024) void norm_held_kernel(Held G, const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                         T* __restrict__ y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
+{
+    extern __shared__ float shared[];                    // per lane (ONE) or lane and channel: mean, m2; then per group: mean, rstd
+    const uint32_t block = held_block(gridDim.x);
+    const uint32_t n = fast_div(block, G.by_chunks);
+    const int c0 = (int)(block - n * (uint32_t)G.chunks) * G.chunk, width = min(G.chunk, G.s.c - c0);
+    const int groups = (int)fast_div((uint32_t)width, G.by_cpg), g0 = (int)fast_div((uint32_t)c0, G.by_cpg);
+    const int ty = (int)fast_div(threadIdx.x, G.by_tx), tx = (int)threadIdx.x - ty * G.tx, c = tx * V;
+    const bool mine = ty < G.ty && c < width;
+    const int pitch = G.tx * V / G.span, all = G.ty * pitch;
+    float* s_mean = shared;
+    float* s_m2 = shared + all;
+    float* g_mean = s_m2 + all;
+    float* g_rstd = g_mean + groups;
+    const int count = mine ? G.runs - (ty >= G.full) : 0;
+    // Without branches, so that all loads are on their way together: what a lane reads past its runs counts as nothing.
+    Kept<T, V> kept[R];
+    // (It is of its own group all the same, so that something not finite stays in there.)
+    const T* from = x + n * G.s.x_image + c0 + (c < width ? c : 0);
+    if (count) from += ty * G.s.x_pixel;
+    const long long step = G.ty * G.s.x_pixel;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        kept[k].load(from);
+        from += k + 1 < count ? step : 0;                // past its last run a lane reads that one again
+    }
+    float mean[ONE ? 1 : V], rstd[ONE ? 1 : V], ga[V], be[V];
+    {
+        // sums, then squared distances from a mean, of what the lane holds, per channel or over its channels.  Folded: the group's mean
+        // (two sums over the workgroup); otherwise the lane's own, and lanes are joined by Chan's formula.
+        constexpr int N = ONE ? (V > 1 ? 2 : 1) : V, M = ONE ? 1 : V;
+        float sum[N], m2[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = m2[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (k < G.runs) {
+                const float counts = k < count ? 1.0f : 0.0f;
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i % N] = fmaf(counts, kept[k].at(i), sum[i % N]);
+            }
+            kept[k].used(sum);
+        }
+        if (ONE && N > 1) sum[0] += sum[N - 1];
+        float* s_part = shared;                          // folded: per wavefront and group; two of them, for the sums and for the squares
+        const int wave = (int)threadIdx.x >> 6, waves = (int)blockDim.x >> 6;
+        const bool folded = ONE && G.folded;
+        if (folded) {
+            sum[0] = fold(G, sum[0], c, groups, wave, waves, s_part) * G.inv_m;
+        } else {
+            const float share = count ? 1.0f / (float)(ONE ? count * V : count) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < M; ++i) sum[i] *= share;
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (k < G.runs) {
+                const float counts = k < count ? 1.0f : 0.0f;
+                float from_mean[M];
+#pragma unroll
+                for (int i = 0; i < M; ++i) from_mean[i] = -counts * sum[i];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float d = fmaf(counts, kept[k].at(i), from_mean[ONE ? 0 : i]);
+                    m2[i % N] = fmaf(d, d, m2[i % N]);
+                }
+            }
+            kept[k].used(m2);
+        }
+        if (ONE && N > 1) m2[0] += m2[N - 1];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            ga[i] = gamma && count ? gamma[c0 + c + i] : 1.0f;
+            be[i] = beta && count ? beta[c0 + c + i] : 0.0f;
+        }
+        if (folded) {
+            m2[0] = fold(G, m2[0], c, groups, wave, waves, s_part + waves * groups);
+            mean[0] = sum[0];
+            rstd[0] = 1.0f / sqrtf(m2[0] * G.inv_m + G.s.eps);
+            const int g = (int)fast_div((uint32_t)c, G.by_cpg);
+            if (ty == 0 && count && c == g * G.cpg) {
+                const long long at = (long long)n * G.s.groups + g0 + g;
+                if (mean_out) mean_out[at] = mean[0];
+                if (rstd_out) rstd_out[at] = rstd[0];
+            }
+        } else {
+            if constexpr (!ONE) {
+                // channels of one group, equally many values each: pairs, then pairs of pairs
+                auto pair = [&](int i, int d) {
+                    const float mid = 0.5f * (sum[i] + sum[i + d]), off = sum[i] - mid;
+                    m2[i] += m2[i + d] + 2.0f * (float)(count * d) * off * off;
+                    sum[i] = mid;
+                };
+                if (G.span >= 2)
+#pragma unroll
+                    for (int i = 0; i < V; i += 2) pair(i, 1);
+                if (G.span >= 4)
+#pragma unroll
+                    for (int i = 0; i + 2 < V; i += 4) pair(i, 2);
+            }
+            if (mine) {
+                int at = ty * pitch + tx * (pitch / G.tx);
+#pragma unroll
+                for (int i = 0; i < M; ++i)
+                    if (ONE || (i & (G.span - 1)) == 0) {
+                        s_mean[at] = sum[i];
+                        s_m2[at] = m2[i];
+                        ++at;
+                    }
+            }
+            __syncthreads();
+            const int lane = (int)threadIdx.x & (G.join - 1);
+            for (int g = (int)threadIdx.x / G.join; g < groups; g += (int)blockDim.x / G.join) {
+                float mean_g, m2_g;
+                join_stats(G.entries * G.ty, lane, G.join, [&](int i, float& ni, float& mi, float& si) {
+                    const int row = (int)fast_div((uint32_t)i, G.by_entries), at = row * pitch + g * G.entries + (i - row * G.entries);
+                    ni = (float)((G.runs - (row >= G.full)) * G.span);
+                    mi = s_mean[at];
+                    si = s_m2[at];
+                }, mean_g, m2_g);
+                if (lane == 0) {
+                    const float rstd_g = 1.0f / sqrtf(m2_g * G.inv_m + G.s.eps);
+                    const long long at = (long long)n * G.s.groups + g0 + g;
+                    g_mean[g] = mean_g;
+                    g_rstd[g] = rstd_g;
+                    if (mean_out) mean_out[at] = mean_g;
+                    if (rstd_out) rstd_out[at] = rstd_g;
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                const int g = count ? (int)fast_div((uint32_t)(c + i), G.by_cpg) : 0;
+                mean[i] = g_mean[g];
+                rstd[i] = g_rstd[g];
+            }
+        }
+    }
+    if (count == 0) return;
+    T* to = y + n * G.s.y_image + ty * G.s.y_pixel + c0 + c;
+    const long long y_step = G.ty * G.s.y_pixel;
+    auto apply = [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (ACT != kActRelu)
+#pragma unroll
+            for (int i = 0; i < V; ++i) straight(mean[ONE ? 0 : i], rstd[ONE ? 0 : i], ga[i], be[i]);
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (k < count) {
+                Pack<T, V> r;
+#pragma unroll
+                for (int i = 0; i < V; ++i) r.v[i] = from_float<T>(apply_one<ACT>(kept[k].at(i), mean[ONE ? 0 : i], rstd[ONE ? 0 : i], ga[i], be[i]));
+                store_pack<T, V>(to, r);
+                to += y_step;
+                __builtin_amdgcn_sched_barrier(0);       // one run's values at a time
+            }
+    };
+    if (G.s.act == kActRelu) apply(Const<kActRelu>{});
+    else if (G.s.act == kActSilu) apply(Const<kActSilu>{});
+    else apply(Const<kActNone>{});
+}
+
 // ---- backward ----
 
-// dz and xh of one value.
-template <int ACT>
-__device__ __forceinline__ void slopes(float x, float dy, float mean, float rstd, float gamma, float beta, float& dz, float& xh)
-{
-    xh = normalised(x, mean, rstd);
-    dz = dy;
-    if (ACT == kActNone) return;
-    const float z = affine(xh, gamma, beta);
-    if (ACT == kActRelu) {
-        dz = z <= 0.0f ? 0.0f : dy;
-    } else {
-        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-        dz = dy * (s * fmaf(z, 1.0f - s, 1.0f));
+// One channel's constants and what the backward pass makes of one value: dz, and d = x - mean, so that xh = d rstd.
+//   dx = rstd (gamma dz - A/M - xh B/M) = dz scale - (shift + d slope)   with scale = rstd gamma, shift = rstd A/M, slope = rstd^2 B/M.
+struct Channel {
+    float mean, rstd, gamma, beta, scale;
+    __device__ __forceinline__ void set(float m, float r, float g, float b) { mean = m, rstd = r, gamma = g, beta = b, scale = r * g; }
+    template <int ACT>
+    __device__ __forceinline__ void slopes(float x, float dy, float& dz, float& d) const
+    {
+        d = centred(x, mean);
+        dz = dy;
+        if (ACT == kActRelu) dz = affine(d, rstd, gamma, beta) <= 0.0f ? 0.0f : dy;       // the forward pass's z
+        if (ACT == kActSilu) {
+            const float z = fmaf(d, scale, beta), s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+            dz = dy * (s * fmaf(z, 1.0f - s, 1.0f));
+        }
     }
-}
+};
 
 // Calls f(x, dy) for every ty-th pixel of the slab.
 template <class T, int V, class F>
@@ -310,30 +573,28 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(Geometry G, co
     const int c = tx * V, pitch = G.tx * V;
     if (ty < G.ty && c < w.width) {
         const int first = w.p0 + ty, count = first < w.p1 ? (w.p1 - first + G.ty - 1) / G.ty : 0;
-        float mean[V], rstd[V], ga[V], be[V], a[V], b[V];
+        Channel ch[V];
+        float a[V], b[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const long long g = (long long)w.n * G.s.groups + w.g0 + (G.per_group == 1 ? (int)fast_div((uint32_t)(c + i), G.by_cpg) : 0);
-            mean[i] = mean_in[g];
-            rstd[i] = rstd_in[g];
-            ga[i] = gamma ? gamma[w.c0 + c + i] : 1.0f;
-            be[i] = beta ? beta[w.c0 + c + i] : 0.0f;
+            ch[i].set(mean_in[g], rstd_in[g], gamma ? gamma[w.c0 + c + i] : 1.0f, beta ? beta[w.c0 + c + i] : 0.0f);
             a[i] = b[i] = 0.0f;
         }
         walk2<T, V>(x + w.n * G.s.x_image + first * G.s.x_pixel + w.c0 + c, G.ty * G.s.x_pixel,
                     dy + w.n * G.s.dy_image + first * G.s.dy_pixel + w.c0 + c, G.ty * G.s.dy_pixel, count, [&](const float (&v)[V], const float (&d)[V]) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                float dz, xh;
-                slopes<ACT>(v[i], d[i], mean[i], rstd[i], ga[i], be[i], dz, xh);
+                float dz, off;
+                ch[i].template slopes<ACT>(v[i], d[i], dz, off);
                 a[i] += dz;
-                b[i] = fmaf(dz, xh, b[i]);
+                b[i] = fmaf(dz, off, b[i]);
             }
         });
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             s_a[ty * pitch + c + i] = a[i];
-            s_b[ty * pitch + c + i] = b[i];
+            s_b[ty * pitch + c + i] = b[i] * ch[i].rstd;
         }
     }
     __syncthreads();
@@ -447,16 +708,15 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(Geometry G, i
     const int ty = (int)fast_div(threadIdx.x, G.by_tx), tx = (int)threadIdx.x - ty * G.tx;
     const int c = tx * V, first = w.p0 + ty;
     if (ty >= G.ty || c >= w.width || first >= w.p1) return;
-    float mean[V], rstd[V], ga[V], be[V], ma[V], mb[V];
+    Channel ch[V];
+    float shift[V], slope[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int g = G.per_group == 1 ? (int)fast_div((uint32_t)(c + i), G.by_cpg) : 0;
-        mean[i] = mean_in[(long long)w.n * G.s.groups + w.g0 + g];
-        rstd[i] = rstd_in[(long long)w.n * G.s.groups + w.g0 + g];
-        ga[i] = gamma ? gamma[w.c0 + c + i] : 1.0f;
-        be[i] = beta ? beta[w.c0 + c + i] : 0.0f;
-        ma[i] = g_a[g];
-        mb[i] = g_b[g];
+        const long long at = (long long)w.n * G.s.groups + w.g0 + g;
+        ch[i].set(mean_in[at], rstd_in[at], gamma ? gamma[w.c0 + c + i] : 1.0f, beta ? beta[w.c0 + c + i] : 0.0f);
+        shift[i] = ch[i].rstd * g_a[g];
+        slope[i] = ch[i].rstd * ch[i].rstd * g_b[g];
     }
     T* to = dx + w.n * G.s.y_image + first * G.s.y_pixel + w.c0 + c;
     walk2<T, V>(x + w.n * G.s.x_image + first * G.s.x_pixel + w.c0 + c, G.ty * G.s.x_pixel,
@@ -465,9 +725,9 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(Geometry G, i
         Pack<T, V> r;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float dz, xh;
-            slopes<ACT>(v[i], d[i], mean[i], rstd[i], ga[i], be[i], dz, xh);
-            r.v[i] = from_float<T>(rstd[i] * (__fsub_rn(__fmul_rn(dz, ga[i]), ma[i]) - xh * mb[i]));
+            float dz, off;
+            ch[i].template slopes<ACT>(v[i], d[i], dz, off);
+            r.v[i] = from_float<T>(fmaf(dz, ch[i].scale, -fmaf(off, slope[i], shift[i])));
         }
         store_pack<T, V>(to, r);
         to += G.ty * G.s.y_pixel;
@@ -505,18 +765,22 @@ Geometry geometry_of(const NormShape& s)
     return G;
 }
 
-// Elements that a lane moves with one access: as many as everything is aligned to.
-int run_of(const Geometry& G, const void* const* pointers, const long long* strides, int count)
+// Elements that a lane moves with one access: as many as everything is aligned to, up to 16 bytes of them.
+int aligned_run(const NormShape& s, const void* const* pointers, const long long* strides, int count)
 {
-    const int bytes = (int)element_bytes(G.s.type);
-    uint64_t all = 0;
+    const int bytes = (int)element_bytes(s.type);
+    uint64_t all = (uint64_t)s.c;
     for (int i = 0; i < count; ++i) all |= reinterpret_cast<uintptr_t>(pointers[i]) / bytes;
     for (int i = 0; i < 2 * count; ++i) all |= (uint64_t)strides[i];
-    all |= (uint64_t)G.s.c;
-    if (G.chunks > 1) all |= (uint64_t)G.chunk;
-    if (G.per_group > 1) all |= (uint64_t)G.cpg;
     int v = 16 / bytes;
     while (all % (uint64_t)v) v /= 2;
+    return v;
+}
+// The same where chunks and slabs are taken.
+int run_of(const Geometry& G, const void* const* pointers, const long long* strides, int count)
+{
+    int v = aligned_run(G.s, pointers, strides, count);
+    while ((G.chunks > 1 && G.chunk % v) || (G.per_group > 1 && G.cpg % v)) v /= 2;
     return v;
 }
 
@@ -524,6 +788,11 @@ void finish(Geometry& G, int v)
 {
     G.tx = (std::min(G.chunk, G.s.c) + v - 1) / v;
     G.ty = kThreads / G.tx;
+    const int last = G.s.pixels - (G.slabs - 1) * G.slab;
+    G.runs = (G.slab + G.ty - 1) / G.ty;
+    G.full = G.slab - (G.runs - 1) * G.ty;
+    G.last_runs = (last + G.ty - 1) / G.ty;
+    G.last_full = last - (G.last_runs - 1) * G.ty;
     G.by_slabs = make_fast_div((uint32_t)G.slabs);
     G.by_chunks = make_fast_div((uint32_t)G.chunks);
     G.by_tx = make_fast_div((uint32_t)G.tx);
@@ -537,6 +806,63 @@ template <class F>
 void with_run(int v, F&& f)
 {
     v == 8 ? f(Const<8>{}) : v == 4 ? f(Const<4>{}) : v == 2 ? f(Const<2>{}) : f(Const<1>{});
+}
+
+// The held kernel's geometry for lanes of `v` channels, up to `most` runs a lane; false if the pixels do not fit.
+bool held_of(const NormShape& s, int v, int most, Held& H, int& threads, int& runs)
+{
+    H = Held{};
+    H.s = s;
+    H.cpg = s.c / s.groups;
+    H.chunk = H.cpg;
+    while (H.chunk % v && H.chunk < s.c) H.chunk += H.cpg;
+    auto fits = [&](int chunk) { return chunk % v == 0 && chunk / v <= 1024 && (s.pixels + 1024 / (chunk / v) - 1) / (1024 / (chunk / v)) <= most; };
+    if (!fits(H.chunk)) return false;
+    // Few bytes a pixel and many pixels: most of each cache line is fetched for others.  (1 x 112x112x64 in groups of two channels, fp16: 29 us
+    // held and 17 in two launches; 64 of them 89 and 69; at 56x56 11 and 15, 18 and 29.)
+    if (H.chunk * element_bytes(s.type) < 32 && s.pixels > 8192) return false;
+    // 64 adjacent bytes a pixel, as long as every CU has a workgroup
+    while (H.chunk * element_bytes(s.type) < 64 && H.chunk * 2 <= s.c && fits(H.chunk * 2) && (long long)s.n * (s.c / (H.chunk * 2)) >= 256) H.chunk *= 2;
+    H.chunks = (s.c + H.chunk - 1) / H.chunk;
+    if ((long long)s.n * H.chunks > kMostBlocks / 4) return false;
+    H.tx = H.chunk / v;
+    // Every lane has one run where there are few workgroups; where there are many, four, and several workgroups share a CU.
+    const long long need = (long long)H.tx * s.pixels / ((long long)s.n * H.chunks >= 512 ? 4 : 1);
+    threads = (int)std::max<long long>((H.tx + 63) / 64 * 64, std::min<long long>(1024, (need + 63) / 64 * 64));
+    H.ty = threads / H.tx;
+    runs = H.runs = (s.pixels + H.ty - 1) / H.ty;
+    H.full = s.pixels - (H.runs - 1) * H.ty;
+    H.inv_m = (float)(1.0 / ((double)s.pixels * H.cpg));
+    H.by_chunks = make_fast_div((uint32_t)H.chunks);
+    H.by_tx = make_fast_div((uint32_t)H.tx);
+    H.by_cpg = make_fast_div((uint32_t)H.cpg);
+    H.span = H.cpg % v == 0 ? v : v % H.cpg == 0 && H.cpg <= 4 ? H.cpg : 1;
+    H.entries = H.lanes = H.cpg / H.span;
+    auto power = [](int i) { return (i & (i - 1)) == 0; };
+    H.folded = H.cpg % v == 0 && H.tx <= 64 && power(H.tx) && power(H.lanes);
+    H.by_entries = make_fast_div((uint32_t)H.entries);
+    H.join = 64;
+    while (H.join > 1 && H.chunk / H.cpg * H.join > threads) H.join /= 2;
+    return true;
+}
+
+size_t held_lds(const Held& H, int v, int threads)
+{
+    const size_t groups = (size_t)H.chunk / H.cpg;
+    return (H.folded ? (size_t)threads / 64 * groups : (size_t)H.ty * H.tx * v / H.span + groups) * 2 * sizeof(float);
+}
+
+template <class T, int V, int R, bool ONE>
+hipError_t launch_held(const Held& H, int threads, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd,
+                       hipStream_t stream)
+{
+    static std::atomic<uint64_t> allowed{0};
+    const size_t lds = held_lds(H, V, threads);
+    if (lds > 64 * 1024)
+        if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(norm_held_kernel<T, V, R, ONE>), allowed); e != hipSuccess) return e;
+    hipLaunchKernelGGL((norm_held_kernel<T, V, R, ONE>), dim3((unsigned)(H.s.n * H.chunks)), dim3((unsigned)threads), lds, stream, H,
+                       static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd);
+    return hipGetLastError();
 }
 
 int param_blocks_of(const NormShape& s) { return (s.c + kParamChannels - 1) / kParamChannels; }
@@ -559,9 +885,39 @@ size_t norm_workspace_floats(const NormShape& s, bool backward)
 hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd,
                        float* workspace, hipStream_t stream)
 {
-    Geometry G = geometry_of(s);
     const void* pointers[] = {x, y};
     const long long strides[] = {s.x_image, s.x_pixel, s.y_image, s.y_pixel};
+    for (int v = aligned_run(s, pointers, strides, 2); v > 0; v /= 2) {
+        hipError_t e = hipErrorNotReady;
+        with_type(s.type, [&](auto t) {
+            using T = decltype(t);
+            with_run(v, [&](auto run) {
+                constexpr int V = decltype(run)::value;
+                if constexpr (V * sizeof(T) <= 16) {
+                    constexpr int kMost = held_runs<T, V>();
+                    Held H;
+                    int threads, runs;
+                    if (!held_of(s, V, kMost, H, threads, runs)) return;
+                    auto with_runs = [&](auto r) {
+                        constexpr int R = decltype(r)::value;
+                        if constexpr (V > 1)
+                            if (H.cpg % V) {
+                                e = launch_held<T, V, R, false>(H, threads, x, gamma, beta, y, mean, rstd, stream);
+                                return;
+                            }
+                        e = launch_held<T, V, R, true>(H, threads, x, gamma, beta, y, mean, rstd, stream);
+                    };
+                    if (runs <= 2) with_runs(Const<2>{});
+                    else if (runs <= kMost / 4) with_runs(Const<kMost / 4>{});
+                    else if (runs <= kMost / 2) with_runs(Const<kMost / 2>{});
+                    else if (runs <= kMost * 3 / 4 + 1) with_runs(Const<kMost * 3 / 4 + 1>{});
+                    else with_runs(Const<kMost>{});
+                }
+            });
+        });
+        if (e != hipErrorNotReady) return e;
+    }
+    Geometry G = geometry_of(s);
     const int v = run_of(G, pointers, strides, 2);
     finish(G, v);
     const dim3 grid((unsigned)(s.n * G.chunks * G.slabs));

@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 256;          // most channels of a chunk
-constexpr int kMostSlabs = 128;
+constexpr int kMostSlabs = 64;
 constexpr int kAhead = 4;            // pixels a lane has in flight
 
 struct Geometry {
@@ -36,8 +36,9 @@ struct Geometry {
     int tx, ty;                      // lanes side by side over channels, and over pixels
     int join;                        // lanes that join the sums of one group (a power of two up to 64)
     int runs, full, last_runs, last_full;        // pixels that the first `full` rows of lanes have, the others one less; of the last slab
+    int width, parts;                // channels of a chunk that is whole, and how often a workgroup has a lane for each
     float inv_m;                     // 1 / (pixels * cpg)
-    FastDiv by_slabs, by_chunks, by_tx, by_cpg;
+    FastDiv by_slabs, by_chunks, by_tx, by_cpg, by_width;
 };
 
 // What a workgroup works on.
@@ -282,7 +283,8 @@ struct Held {
     int folded, lanes;                                   // a group's lanes in a row are a power of two (`lanes`), and the rows too: sums fold by exchange
     int runs, full;                                      // runs that the first `full` rows of lanes have, the others one less
     float inv_m;
-    FastDiv by_chunks, by_tx, by_cpg, by_entries;
+    int parts;                                           // into which the backward kernel cuts the rows of lanes where it adds columns up
+    FastDiv by_chunks, by_tx, by_cpg, by_entries, by_chunk;
 };
 
 // Most runs that a lane holds: 64 registers of them (32 of one or two bytes).
@@ -311,6 +313,11 @@ struct Kept {
         } else {
             w[0] = *reinterpret_cast<const unsigned short*>(p);
         }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
     }
     __device__ __forceinline__ float at(int i) const
     {
@@ -611,7 +618,257 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(Geometry G, co
     }
 }
 
-constexpr int kParamChannels = 16;       // channels of a workgroup that adds up dgamma and dbeta
+// Sums over images (and slabs) of parts [row][2][channel] -> dbeta, dgamma, kParamChannels channels a workgroup.
+constexpr int kParamChannels = 16;
+__device__ __forceinline__ void add_params(int channels, long long rows, int first, const float* __restrict__ parts, float* s_a, float* s_b,
+                                           float* __restrict__ dgamma, float* __restrict__ dbeta)
+{
+    constexpr int kRows = kThreads / kParamChannels;
+    const int i = (int)threadIdx.x % kParamChannels, row = (int)threadIdx.x / kParamChannels, c = first + i;
+    float a = 0.0f, b = 0.0f;
+    if (c < channels)
+        for (long long k = row; k < rows; k += kRows) {
+            a += parts[k * 2 * channels + c];
+            b += parts[(k * 2 + 1) * channels + c];
+        }
+    s_a[threadIdx.x] = a;
+    s_b[threadIdx.x] = b;
+    __syncthreads();
+    if (row == 0 && c < channels) {
+        for (int k = 1; k < kRows; ++k) {
+            a += s_a[k * kParamChannels + i];
+            b += s_b[k * kParamChannels + i];
+        }
+        if (dbeta) dbeta[c] = a;
+        if (dgamma) dgamma[c] = b;
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void norm_params_kernel(int channels, int images, const float* __restrict__ parts, float* __restrict__ dgamma,
+                                                               float* __restrict__ dbeta)
+{
+    __shared__ float s_a[kThreads], s_b[kThreads];
+    add_params(channels, images, (int)blockIdx.x * kParamChannels, parts, s_a, s_b, dgamma, dbeta);
+}
+
+// Runs of dy that the kernel below keeps in LDS.
+template <int R>
+constexpr int held_in_lds() { return R > 8 ? 9 : 0; }
+
+// The backward pass of what norm_held_kernel does.  x and dy are both held: R runs of either, of dy the first held_in_lds<R>() in LDS.
+// sums: [image][2][channel], dz and dz xh over the image's pixels.
+template <class T, int V, int R, bool ONE>
+__global__ __launch_bounds__(1024) void norm_back_held_kernel(Held G, const T* __restrict__ dy, const T* __restrict__ x, const float* __restrict__ mean_in,
+                                                              const float* __restrict__ rstd_in, const float* __restrict__ gamma,
+                                                              const float* __restrict__ beta, T* __restrict__ dx, float* __restrict__ sums)
+{
+    constexpr int kInLds = held_in_lds<R>(), M = ONE ? 1 : V;
+    using Run = Kept<T, V>;
+    extern __shared__ float shared[];
+    const uint32_t block = held_block(gridDim.x);
+    const uint32_t n = fast_div(block, G.by_chunks);
+    const int c0 = (int)(block - n * (uint32_t)G.chunks) * G.chunk, width = min(G.chunk, G.s.c - c0);
+    const int groups = (int)fast_div((uint32_t)width, G.by_cpg), g0 = (int)fast_div((uint32_t)c0, G.by_cpg);
+    const int ty = (int)fast_div(threadIdx.x, G.by_tx), tx = (int)threadIdx.x - ty * G.tx, c = tx * V;
+    const bool mine = ty < G.ty && c < width;
+    const int threads = (int)blockDim.x, wave = (int)threadIdx.x >> 6, waves = threads >> 6;
+    const int count = mine ? G.runs - (ty >= G.full) : 0;
+    const int inside = c < width ? c : 0;
+    Run* const s_dy = reinterpret_cast<Run*>(shared) + threadIdx.x;      // [run][thread]
+    float* const s = shared + kInLds * threads * Run::kWords;
+    // As in the forward kernel: no branches, what a lane reads past its runs counts as nothing.
+    Run kx[R], kd[R - kInLds];
+    {
+        const T* px = x + n * G.s.x_image + c0 + inside;
+        const T* pd = dy + n * G.s.dy_image + c0 + inside;
+        if (count) px += ty * G.s.x_pixel, pd += ty * G.s.dy_pixel;
+        const long long x_step = G.ty * G.s.x_pixel, d_step = G.ty * G.s.dy_pixel;
+        Run first[kInLds ? kInLds : 1];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (k < kInLds) first[k < kInLds ? k : 0].load(pd);
+            else kd[k < kInLds ? 0 : k - kInLds].load(pd);
+            pd += k + 1 < count ? d_step : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            kx[k].load(px);
+            px += k + 1 < count ? x_step : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kInLds; ++k) s_dy[k * threads] = first[k];      // read by this thread only
+    }
+    float mean[M], rstd[M], ga[V], be[V], a[V], b[V];
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        const long long g = (long long)n * G.s.groups + g0 + (int)fast_div((uint32_t)(inside + i), G.by_cpg);
+        mean[i] = mean_in[g];
+        rstd[i] = rstd_in[g];
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        ga[i] = gamma ? gamma[c0 + inside + i] : 1.0f;
+        be[i] = beta ? beta[c0 + inside + i] : 0.0f;
+        a[i] = b[i] = 0.0f;
+    }
+    auto channel = [&](int i) {
+        Channel ch;
+        ch.set(mean[ONE ? 0 : i], rstd[ONE ? 0 : i], ga[i], be[i]);
+        return ch;
+    };
+    // dz and d of a run; the branch on the activation is inside so that the runs stay in the same registers
+    auto slopes = [&](const Run& x_run, const Run& d_run, float (&dz)[V], float (&off)[V]) {
+        auto each = [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) channel(i).template slopes<decltype(act)::value>(x_run.at(i), d_run.at(i), dz[i], off[i]);
+        };
+        if (G.s.act == kActRelu) each(Const<kActRelu>{});
+        else if (G.s.act == kActSilu) each(Const<kActSilu>{});
+        else each(Const<kActNone>{});
+    };
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        if (k < G.runs) {
+            Run d = k < kInLds ? s_dy[k * threads] : kd[k < kInLds ? 0 : k - kInLds];
+            if (k >= count) d.clear();
+            float dz[V], off[V];
+            slopes(kx[k], d, dz, off);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                a[i] += dz[i];
+                b[i] = fmaf(dz[i], off[i], b[i]);
+            }
+        }
+        kx[k].used(b);
+        if (k >= kInLds) kd[k < kInLds ? 0 : k - kInLds].used(a);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] *= rstd[ONE ? 0 : i];
+
+    float* const to = sums + (long long)n * 2 * G.s.c + c0;
+    float shift[M], slope[M];                            // of Channel's comment
+    if (ONE && G.folded) {
+        // over the rows of lanes of a wavefront by exchange, then the wavefronts; a group's sums likewise
+        float ag = 0.0f, bg = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            for (int d = G.tx; d < 64; d *= 2) {
+                a[i] += __shfl_xor(a[i], d, 64);
+                b[i] += __shfl_xor(b[i], d, 64);
+            }
+            ag = fmaf(ga[i], a[i], ag);
+            bg = fmaf(ga[i], b[i], bg);
+        }
+        for (int d = 1; d < G.lanes; d *= 2) {
+            ag += __shfl_xor(ag, d, 64);
+            bg += __shfl_xor(bg, d, 64);
+        }
+        float* const s_group = s;                        // [wave][2][group]
+        float* const s_channel = s + waves * 2 * groups; // [wave][2][channel]
+        const int g = (int)fast_div((uint32_t)inside, G.by_cpg);
+        if (((int)threadIdx.x & 63) < G.tx && c < width) {
+            s_group[(wave * 2) * groups + g] = ag;
+            s_group[(wave * 2 + 1) * groups + g] = bg;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                s_channel[(wave * 2) * G.chunk + c + i] = a[i];
+                s_channel[(wave * 2 + 1) * G.chunk + c + i] = b[i];
+            }
+        }
+        __syncthreads();
+        ag = bg = 0.0f;
+        for (int k = 0; k < waves; ++k) {
+            ag += s_group[(k * 2) * groups + g];
+            bg += s_group[(k * 2 + 1) * groups + g];
+        }
+        for (int i = (int)threadIdx.x; i < 2 * G.chunk; i += threads) {
+            const int half = i >= G.chunk, at = i - half * G.chunk;
+            float v = 0.0f;
+            for (int k = 0; k < waves; ++k) v += s_channel[(k * 2 + half) * G.chunk + at];
+            if (at < width) to[half * G.s.c + at] = v;
+        }
+        shift[0] = rstd[0] * (ag * G.inv_m);
+        slope[0] = rstd[0] * rstd[0] * (bg * G.inv_m);
+    } else {
+        const int pitch = G.tx * V, all = G.ty * pitch;
+        float* const s_a = s;                            // [row of lanes][channel]
+        float* const s_b = s + all;
+        if (ty < G.ty) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                s_a[ty * pitch + c + i] = a[i];
+                s_b[ty * pitch + c + i] = b[i];
+            }
+        }
+        __syncthreads();
+        // columns: in parts of the rows, then the parts; the totals, weighted with gamma, stay in the first row
+        float* const s_part = s + 2 * all;               // [part][2][channel]
+        const int part = (int)fast_div(threadIdx.x, G.by_chunk);
+        for (int i = part < G.parts ? (int)threadIdx.x - part * pitch : pitch; i < pitch; i += threads) {
+            float pa = 0.0f, pb = 0.0f;
+            for (int k = part; k < G.ty; k += G.parts) {
+                pa += s_a[k * pitch + i];
+                pb += s_b[k * pitch + i];
+            }
+            s_part[(part * 2) * pitch + i] = pa;
+            s_part[(part * 2 + 1) * pitch + i] = pb;
+        }
+        __syncthreads();
+        for (int i = (int)threadIdx.x; i < width; i += threads) {
+            float pa = 0.0f, pb = 0.0f;
+            for (int k = 0; k < G.parts; ++k) {
+                pa += s_part[(k * 2) * pitch + i];
+                pb += s_part[(k * 2 + 1) * pitch + i];
+            }
+            to[i] = pa;
+            to[G.s.c + i] = pb;
+            const float weight = gamma ? gamma[c0 + i] : 1.0f;
+            s_a[i] = weight * pa;
+            s_b[i] = weight * pb;
+        }
+        __syncthreads();
+        float* const g_a = s_part;                       // per group
+        float* const g_b = s_part + groups;
+        const int lane = (int)threadIdx.x & (G.join - 1);
+        for (int g = (int)threadIdx.x / G.join; g < groups; g += threads / G.join) {
+            float ag = 0.0f, bg = 0.0f;
+            for (int i = lane; i < G.cpg; i += G.join) {
+                ag += s_a[g * G.cpg + i];
+                bg += s_b[g * G.cpg + i];
+            }
+            ag = lanes_sum(ag, G.join);
+            bg = lanes_sum(bg, G.join);
+            if (lane == 0) {
+                g_a[g] = ag * G.inv_m;
+                g_b[g] = bg * G.inv_m;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const int g = (int)fast_div((uint32_t)(inside + i), G.by_cpg);
+            shift[i] = rstd[i] * g_a[g];
+            slope[i] = rstd[i] * rstd[i] * g_b[g];
+        }
+    }
+    if (count == 0) return;
+    T* out = dx + n * G.s.y_image + ty * G.s.y_pixel + c0 + c;
+    const long long step = G.ty * G.s.y_pixel;
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+        if (k < count) {
+            const Run d = k < kInLds ? s_dy[k * threads] : kd[k < kInLds ? 0 : k - kInLds];
+            float dz[V], off[V];
+            slopes(kx[k], d, dz, off);
+            Pack<T, V> r;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                r.v[i] = from_float<T>(fmaf(dz[i], channel(i).scale, -fmaf(off[i], slope[ONE ? 0 : i], shift[ONE ? 0 : i])));
+            store_pack<T, V>(out, r);
+            out += step;
+            __builtin_amdgcn_sched_barrier(0);           // one run's values at a time
+        }
+}
 
 // The first `param_blocks` workgroups add the slabs of all images up to dgamma and dbeta, the others apply.
 template <class T, int V, int ACT>
@@ -623,42 +880,36 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(Geometry G, i
 {
     __shared__ float s_a[kThreads], s_b[kThreads];
     if ((int)blockIdx.x < param_blocks) {
-        constexpr int kRows = kThreads / kParamChannels;
-        const int i = (int)threadIdx.x % kParamChannels, row = (int)threadIdx.x / kParamChannels;
-        const int c = (int)blockIdx.x * kParamChannels + i;
-        float a = 0.0f, b = 0.0f;
-        if (c < G.s.c)
-            for (long long k = row; k < (long long)G.s.n * G.slabs; k += kRows) {
-                a += parts[k * 2 * G.s.c + c];
-                b += parts[(k * 2 + 1) * G.s.c + c];
-            }
-        s_a[threadIdx.x] = a;
-        s_b[threadIdx.x] = b;
-        __syncthreads();
-        if (row == 0 && c < G.s.c) {
-            for (int k = 1; k < kRows; ++k) {
-                a += s_a[k * kParamChannels + i];
-                b += s_b[k * kParamChannels + i];
-            }
-            if (dbeta) dbeta[c] = a;
-            if (dgamma) dgamma[c] = b;
-        }
+        add_params(G.s.c, (long long)G.s.n * G.slabs, (int)blockIdx.x * kParamChannels, parts, s_a, s_b, dgamma, dbeta);
         return;
     }
     const Place w = place_of(G, blockIdx.x - (uint32_t)param_blocks);
     const float* from = parts + (long long)w.n * G.slabs * 2 * G.s.c;
     __shared__ float g_a[kChunk], g_b[kChunk];           // per group of the chunk: A / M, B / M
     if (G.per_group == 1) {
-        if ((int)threadIdx.x < w.width) {                // kThreads >= kChunk
-            const int c = w.c0 + (int)threadIdx.x;
-            float a = 0.0f, b = 0.0f;
-            for (int k = 0; k < G.slabs; ++k) {
-                a += from[(long long)k * 2 * G.s.c + c];
-                b += from[((long long)k * 2 + 1) * G.s.c + c];
+        // channels side by side, the slabs in as many parts as there are lanes for (kThreads >= kChunk)
+        const int part = (int)fast_div(threadIdx.x, G.by_width), i = (int)threadIdx.x - part * G.width;
+        float a = 0.0f, b = 0.0f;
+        if (part < G.parts && i < w.width) {
+            const float* p = from + (long long)part * 2 * G.s.c + w.c0 + i;
+            const long long step = (long long)G.parts * 2 * G.s.c;
+#pragma unroll 4
+            for (int k = part; k < G.slabs; k += G.parts, p += step) {
+                a += p[0];
+                b += p[G.s.c];
             }
-            const float ga = gamma ? gamma[c] : 1.0f;
-            s_a[threadIdx.x] = ga * a;
-            s_b[threadIdx.x] = ga * b;
+        }
+        s_a[threadIdx.x] = a;
+        s_b[threadIdx.x] = b;
+        __syncthreads();
+        if (part == 0 && i < w.width) {
+            for (int k = 1; k < G.parts; ++k) {
+                a += s_a[k * G.width + i];
+                b += s_b[k * G.width + i];
+            }
+            const float ga = gamma ? gamma[w.c0 + i] : 1.0f;
+            s_a[i] = ga * a;
+            s_b[i] = ga * b;
         }
         __syncthreads();
         const int lane = (int)threadIdx.x & (G.join - 1);
@@ -755,9 +1006,9 @@ Geometry geometry_of(const NormShape& s)
         G.per_group = 1;
         G.chunks = (s.c + G.chunk - 1) / G.chunk;
     }
-    // eight workgroups a CU if the slabs keep 32 pixels
-    const long long want = 8 * 256 / std::max<long long>(1, (long long)s.n * G.chunks);
-    const int most = (int)std::min<long long>(kMostSlabs, (s.pixels + 31) / 32);
+    // four workgroups a CU if the slabs keep 64 pixels: every workgroup of the second launch adds up all slabs of its image
+    const long long want = 4 * 256 / std::max<long long>(1, (long long)s.n * G.chunks);
+    const int most = (int)std::min<long long>(kMostSlabs, (s.pixels + 63) / 64);
     G.slabs = (int)std::max<long long>(1, std::min<long long>(want, most));
     G.slab = (s.pixels + G.slabs - 1) / G.slabs;
     G.slabs = (s.pixels + G.slab - 1) / G.slab;
@@ -788,6 +1039,9 @@ void finish(Geometry& G, int v)
 {
     G.tx = (std::min(G.chunk, G.s.c) + v - 1) / v;
     G.ty = kThreads / G.tx;
+    G.width = std::min(G.chunk, G.s.c);
+    G.parts = kThreads / G.width;
+    G.by_width = make_fast_div((uint32_t)G.width);
     const int last = G.s.pixels - (G.slabs - 1) * G.slab;
     G.runs = (G.slab + G.ty - 1) / G.ty;
     G.full = G.slab - (G.runs - 1) * G.ty;
@@ -809,7 +1063,7 @@ void with_run(int v, F&& f)
 }
 
 // The held kernel's geometry for lanes of `v` channels, up to `most` runs a lane; false if the pixels do not fit.
-bool held_of(const NormShape& s, int v, int most, Held& H, int& threads, int& runs)
+bool held_of(const NormShape& s, int v, int most, bool backward, Held& H, int& threads, int& runs)
 {
     H = Held{};
     H.s = s;
@@ -819,15 +1073,16 @@ bool held_of(const NormShape& s, int v, int most, Held& H, int& threads, int& ru
     auto fits = [&](int chunk) { return chunk % v == 0 && chunk / v <= 1024 && (s.pixels + 1024 / (chunk / v) - 1) / (1024 / (chunk / v)) <= most; };
     if (!fits(H.chunk)) return false;
     // Few bytes a pixel and many pixels: most of each cache line is fetched for others.  (1 x 112x112x64 in groups of two channels, fp16: 29 us
-    // held and 17 in two launches; 64 of them 89 and 69; at 56x56 11 and 15, 18 and 29.)
-    if (H.chunk * element_bytes(s.type) < 32 && s.pixels > 8192) return false;
+    // held and 17 in two launches; 64 of them 89 and 69; at 56x56 11 and 15, 18 and 29.  Backward 32 x 90x90x128 in groups of four, fp32: 183 and 163.)
+    if (H.chunk * element_bytes(s.type) < 32 && s.pixels > (backward ? 4096 : 8192)) return false;
     // 64 adjacent bytes a pixel, as long as every CU has a workgroup
     while (H.chunk * element_bytes(s.type) < 64 && H.chunk * 2 <= s.c && fits(H.chunk * 2) && (long long)s.n * (s.c / (H.chunk * 2)) >= 256) H.chunk *= 2;
     H.chunks = (s.c + H.chunk - 1) / H.chunk;
     if ((long long)s.n * H.chunks > kMostBlocks / 4) return false;
     H.tx = H.chunk / v;
-    // Every lane has one run where there are few workgroups; where there are many, four, and several workgroups share a CU.
-    const long long need = (long long)H.tx * s.pixels / ((long long)s.n * H.chunks >= 512 ? 4 : 1);
+    // Every lane has one run where there are few workgroups; where there are many, four (eight where x and dy are held), and several
+    // workgroups share a CU.  (64 x 14x14x1024 fp16: 34 us with one run a lane, 16 with four.)
+    const long long need = (long long)H.tx * s.pixels / ((long long)s.n * H.chunks < 512 ? 1 : std::min(most, backward ? 8 : 4));
     threads = (int)std::max<long long>((H.tx + 63) / 64 * 64, std::min<long long>(1024, (need + 63) / 64 * 64));
     H.ty = threads / H.tx;
     runs = H.runs = (s.pixels + H.ty - 1) / H.ty;
@@ -841,6 +1096,8 @@ bool held_of(const NormShape& s, int v, int most, Held& H, int& threads, int& ru
     auto power = [](int i) { return (i & (i - 1)) == 0; };
     H.folded = H.cpg % v == 0 && H.tx <= 64 && power(H.tx) && power(H.lanes);
     H.by_entries = make_fast_div((uint32_t)H.entries);
+    H.parts = std::max(1, threads / H.chunk);
+    H.by_chunk = make_fast_div((uint32_t)H.chunk);
     H.join = 64;
     while (H.join > 1 && H.chunk / H.cpg * H.join > threads) H.join /= 2;
     return true;
@@ -862,6 +1119,28 @@ hipError_t launch_held(const Held& H, int threads, const void* x, const float* g
         if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(norm_held_kernel<T, V, R, ONE>), allowed); e != hipSuccess) return e;
     hipLaunchKernelGGL((norm_held_kernel<T, V, R, ONE>), dim3((unsigned)(H.s.n * H.chunks)), dim3((unsigned)threads), lds, stream, H,
                        static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd);
+    return hipGetLastError();
+}
+
+// The backward kernel's LDS: held runs of dy; where sums fold, per wavefront those of groups and channels, else those of every lane and
+// of the parts of the rows.
+size_t held_back_lds(const Held& H, int v, int threads, int in_lds, size_t run_bytes)
+{
+    const size_t groups = (size_t)H.chunk / H.cpg;
+    const size_t floats = H.folded ? (size_t)threads / 64 * 2 * (groups + H.chunk) : 2 * (size_t)H.ty * H.chunk + std::max<size_t>(2 * (size_t)H.parts * H.chunk, 2 * groups);
+    return (size_t)in_lds * threads * run_bytes + floats * sizeof(float);
+}
+
+template <class T, int V, int R, bool ONE>
+hipError_t launch_held_back(const Held& H, int threads, const void* dy, const void* x, const float* mean, const float* rstd, const float* gamma,
+                            const float* beta, void* dx, float* sums, hipStream_t stream)
+{
+    static std::atomic<uint64_t> allowed{0};
+    const size_t lds = held_back_lds(H, V, threads, held_in_lds<R>(), sizeof(Kept<T, V>));
+    if (lds > 64 * 1024)
+        if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(norm_back_held_kernel<T, V, R, ONE>), allowed); e != hipSuccess) return e;
+    hipLaunchKernelGGL((norm_back_held_kernel<T, V, R, ONE>), dim3((unsigned)(H.s.n * H.chunks)), dim3((unsigned)threads), lds, stream, H,
+                       static_cast<const T*>(dy), static_cast<const T*>(x), mean, rstd, gamma, beta, static_cast<T*>(dx), sums);
     return hipGetLastError();
 }
 
@@ -897,7 +1176,7 @@ hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, co
                     constexpr int kMost = held_runs<T, V>();
                     Held H;
                     int threads, runs;
-                    if (!held_of(s, V, kMost, H, threads, runs)) return;
+                    if (!held_of(s, V, kMost, false, H, threads, runs)) return;
                     auto with_runs = [&](auto r) {
                         constexpr int R = decltype(r)::value;
                         if constexpr (V > 1)
@@ -946,9 +1225,45 @@ hipError_t launch_norm_backward(const NormShape& s, const void* dy, const void* 
         if (dbeta && (e = launch_fill_zero(dbeta, (size_t)s.c, stream)) != hipSuccess) return e;
         return hipSuccess;
     }
-    Geometry G = geometry_of(s);
     const void* pointers[] = {x, dx, dy};
     const long long strides[] = {s.x_image, s.x_pixel, s.y_image, s.y_pixel, s.dy_image, s.dy_pixel};
+    // Held where lanes have whole runs of 16 bytes, and sums fold or pixels are few: the other way to add columns up costs more than reading
+    // twice (8 x 56x56x64 in groups of two, fp32: 23 us and 15).
+    e = hipErrorNotReady;
+    with_type(s.type, [&](auto t) {
+        using T = decltype(t);
+        constexpr int V = 16 / (int)sizeof(T);
+        // two-byte values: eight runs take as long as reading twice where thirteen do not fit the registers any more
+        constexpr int kMost = sizeof(T) == 4 ? 13 : 8;
+        if (aligned_run(s, pointers, strides, 3) != V) return;
+        Held H;
+        int threads, runs;
+        const int fewer = s.c / s.groups % V == 0 ? kMost : sizeof(T) == 4 ? 8 : 4;      // more constants a lane: fewer runs
+        // (64 x 56x56x256 bf16, 32 bytes a pixel: 135 us held, 118 in two launches)
+        if (!held_of(s, V, fewer, true, H, threads, runs) || (!H.folded && (s.pixels > 1024 || runs > 8)) ||
+            (H.chunk * sizeof(T) < 64 && (long long)s.n * H.chunks >= 256) ||
+            held_back_lds(H, V, threads, runs > 8 ? held_in_lds<kMost>() : 0, sizeof(Kept<T, V>)) > 160 * 1024)
+            return;
+        auto with_runs = [&](auto r) {
+            constexpr int R = decltype(r)::value;
+            if constexpr (R <= (sizeof(T) == 4 ? 8 : 4))
+                if (H.cpg % V) {
+                    e = launch_held_back<T, V, R, false>(H, threads, dy, x, mean, rstd, gamma, beta, dx, workspace, stream);
+                    return;
+                }
+            e = launch_held_back<T, V, R, true>(H, threads, dy, x, mean, rstd, gamma, beta, dx, workspace, stream);
+        };
+        if (runs <= 2) with_runs(Const<2>{});
+        else if (runs <= 4) with_runs(Const<4>{});
+        else if (runs <= 8) with_runs(Const<8>{});
+        else with_runs(Const<kMost>{});
+    });
+    if (e == hipSuccess && (dgamma || dbeta)) {
+        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)param_blocks_of(s)), dim3(kThreads), 0, stream, s.c, s.n, workspace, dgamma, dbeta);
+        e = hipGetLastError();
+    }
+    if (e != hipErrorNotReady) return e;
+    Geometry G = geometry_of(s);
     const int v = run_of(G, pointers, strides, 3);
     finish(G, v);
     const unsigned blocks = (unsigned)(s.n * G.chunks * G.slabs);

@@ -489,18 +489,26 @@ def patdnn_destroy(handle: Optional[int]) -> None:
 # what stands between and behind the convolutions: order of channels, group norm, MXFP4
 # ---------------------------------------------------------------------------
 
-_types = None
+_modules = {}
+_types = {}
+
+
+def _torch():
+    if not _modules:
+        import torch
+        _modules["torch"] = torch
+        _types.update({torch.float32: PATDNN_F32, torch.float16: PATDNN_F16, torch.bfloat16: PATDNN_BF16})
+    return _modules["torch"]
 
 
 def _type(dtype) -> int:
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: PATDNN_F32, torch.float16: PATDNN_F16, torch.bfloat16: PATDNN_BF16}
-    try:
-        return _types[dtype]
-    except KeyError:
-        raise ValueError(f"float32, float16 or bfloat16 expected, not {dtype}") from None
+    kind = _types.get(dtype)
+    if kind is None:
+        _torch()
+        kind = _types.get(dtype)
+        if kind is None:
+            raise ValueError(f"float32, float16 or bfloat16 expected, not {dtype}")
+    return kind
 
 
 def _act(act: str) -> int:
@@ -513,22 +521,23 @@ def _act(act: str) -> int:
 def _new(shape, dtype, like, stream):
     """A tensor that the call's stream owns: what is allocated while another one is current may not be in use there
     any more before it is here, nor free here before it is there."""
-    import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
+    torch = _torch()
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream(like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _float_vector(t, count: int, name: str) -> Optional[int]:
     if t is None:
         return None
-    import torch
-    if t.dtype != torch.float32 or t.numel() != count:
+    if _types.get(t.dtype) != PATDNN_F32 or t.numel() != count:
         raise ValueError(f"{name} must be float32 with {count} elements")
-    return _devptr(t)
+    if not (t.is_cuda and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    return t.data_ptr()
 
 
 def _channels_last_layout(t, name: str):
@@ -536,13 +545,14 @@ def _channels_last_layout(t, name: str):
     if not t.is_cuda:
         raise ValueError("device tensor expected")
     shape, strides = t.shape, t.stride()
-    if len(shape) < 3:
+    dims = len(shape)
+    if dims < 3:
         raise ValueError(f"{name} must be [n, ..., channels]")
     c = shape[-1]
     if c > 1 and strides[-1] != 1 and t.numel():
         raise ValueError(f"the channels of {name} must be adjacent")
     pixel, pixels = strides[-2], shape[-2]
-    for i in range(len(shape) - 3, 0, -1):
+    for i in range(dims - 3, 0, -1):
         if pixels == 1:
             pixel = strides[i]
         elif shape[i] > 1 and strides[i] != pixel * pixels and t.numel():
@@ -582,7 +592,7 @@ def patdnn_channels_first(x, out=None, *, dtype=None, stream=None):
 
 
 def _norm_workspace(desc, backward: int, workspace, like, stream):
-    import torch
+    torch = _torch()
     floats = lib().patdnn_group_norm_workspace_floats(ctypes.byref(desc), backward)
     if workspace is None:
         workspace = _new((floats,), torch.float32, like, stream)
@@ -595,7 +605,7 @@ def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e
                       stream=None):
     """x [n, ..., c] channels last -> (act(group norm) like x, mean, rstd float32 [n, groups]).  gamma, beta: float32 [c] or None.
     x and ``out`` may be slices of the channels of wider tensors."""
-    import torch
+    torch = _torch()
     n, pixels, c, x_image, x_pixel = _channels_last_layout(x, "x")
     if out is None:
         out = _new(tuple(x.shape), x.dtype, x, stream)
@@ -617,7 +627,7 @@ def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e
 def patdnn_group_norm_backward(dy, x, mean, rstd, groups: int, gamma=None, beta=None, out=None, *, act="none", dgamma=None, dbeta=None,
                                workspace=None, stream=None):
     """Gradients of patdnn_group_norm: (dx like x, dgamma, dbeta float32 [c]) from dy, x and the forward call's mean and rstd."""
-    import torch
+    torch = _torch()
     n, pixels, c, x_image, x_pixel = _channels_last_layout(x, "x")
     if dy.shape != x.shape or dy.dtype != x.dtype:
         raise ValueError("dy must have the shape and type of x")
@@ -653,7 +663,7 @@ def _rows(t, name: str) -> int:
 
 
 def _codes(codes, scales, rows: int, cols: int):
-    import torch
+    torch = _torch()
     pieces = -(-cols // 128)
     if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.shape != (rows, pieces * 64) or scales.shape != (rows, pieces * 4):
         raise ValueError(f"codes and scales must be uint8 {(rows, pieces * 64)} and {(rows, pieces * 4)}")
@@ -662,7 +672,7 @@ def _codes(codes, scales, rows: int, cols: int):
 
 def patdnn_mxfp4_quantize(x, codes=None, scales=None, *, stream=None):
     """x [rows, cols] -> (codes uint8 [rows, ceil(cols/128)*64], scales uint8 [rows, ceil(cols/128)*4])."""
-    import torch
+    torch = _torch()
     row = _rows(x, "x")
     rows, cols = x.shape
     pieces = -(-cols // 128)
@@ -677,7 +687,7 @@ def patdnn_mxfp4_quantize(x, codes=None, scales=None, *, stream=None):
 
 def patdnn_mxfp4_dequantize(codes, scales, cols: int, out=None, *, dtype=None, stream=None):
     """The values [rows, cols] that codes and scales stand for, float32 unless ``out`` or ``dtype`` says otherwise."""
-    import torch
+    torch = _torch()
     rows = codes.shape[0]
     cp, sp = _codes(codes, scales, rows, cols)
     if out is None:
@@ -692,7 +702,7 @@ def patdnn_mxfp4_dequantize(codes, scales, cols: int, out=None, *, dtype=None, s
 def patdnn_mxfp4_linear(x, w, w_scales, bias=None, out=None, *, x_scales=None, act="none", dtype=None, workspace=None, stream=None):
     """x [rows, in] times MXFP4 weights [out, in], plus bias (float32 [out]), activated.  x is float32 / float16 / bfloat16, or the codes
     of patdnn_mxfp4_quantize with ``x_scales``.  The result's type: ``out``'s, ``dtype``, or x's (float32 for codes)."""
-    import torch
+    torch = _torch()
     row = _rows(x, "x")
     features = w.shape[0]
     if x_scales is None:

@@ -5,8 +5,9 @@
 // rows lie in memory.  The weights are the instruction's first operand, so that a lane's four results are
 // neighbours along n.  Sums are fp32.
 //
-// This kernel reads both operands straight from memory: a wavefront takes a range of k for a set of NT x MT tiles of 16 x 16 outputs,
-// and the workgroup's wavefronts add their sums up in LDS, in the order of the ranges.
+// Few rows: the weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs; its wavefronts
+// take pieces of 128 values of k in turn and add their sums up in LDS, in their order.  A wavefront asks for its first weights, then x is
+// quantised into LDS by all of them (every workgroup does that for itself: there is no launch before), and then weights stream through registers.
 #include <type_traits>
 
 #include "linear.hpp"
@@ -17,106 +18,129 @@ namespace {
 
 struct Codes {};                                         // x is MXFP4 already
 
+constexpr int kRows = 16;                                // most rows of x here: the matrix instruction's
+constexpr int kAhead = 8;                                // pieces of weights that a wavefront has on their way
+constexpr int kRowsLds = 128 * 1024;                     // most bytes of x in LDS
+
 struct Args {
     LinearShape s;
-    int pieces;                                          // of 128 along k
-    int n_tiles, m_tiles;                                // workgroups over the outputs
+    int pieces, row_tiles;                               // of 128 along k; of kRows rows of x
     bool whole_runs;                                     // rows of x in runs of 16 bytes
-    FastDiv by_n;
+    FastDiv by_tiles, by_lanes;                          // row_tiles; runs of eight values in a row of x
 };
 
-// This lane's block of 32 values of row m: codes and scale byte.
 template <class X>
-__device__ __forceinline__ void block_of(const Args& A, const void* x, const uint8_t* x_scales, int m, int piece, int kb, uint4& codes, uint32_t& scale)
+__global__ __launch_bounds__(1024) void linear_rows_kernel(Args A, const void* __restrict__ x, const uint8_t* __restrict__ x_scales,
+                                                           const uint8_t* __restrict__ w, const uint8_t* __restrict__ w_scales,
+                                                           const float* __restrict__ bias, void* __restrict__ out)
 {
-    if constexpr (std::is_same_v<X, Codes>) {
-        const long long row = (long long)m * A.pieces + piece;
-        codes = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(x) + row * 64 + kb * 16);
-        scale = x_scales[row * 4 + kb];
-    } else {
-        const int k = piece * 128 + kb * 32;
-        const X* p = static_cast<const X*>(x) + (long long)m * A.s.x_row + k;
-        Pack<X, 8> a[4];
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            a[i] = load8(p + 8 * i, A.s.in - k - 8 * i, A.whole_runs);
-            top = max(top, largest(a[i]));
-        }
-        scale = scale_byte(top);
-        const float unit = scale_of(scale);
-        const bool fine = scale != kNanScale;
-        codes = make_uint4(fine ? encode8(a[0], unit) : 0u, fine ? encode8(a[1], unit) : 0u, fine ? encode8(a[2], unit) : 0u,
-                           fine ? encode8(a[3], unit) : 0u);
-    }
-}
-
-template <class X, int NT, int MT>
-__global__ __launch_bounds__(NT * MT > 1 ? 256 : 1024) void linear_direct_kernel(Args A, const void* __restrict__ x, const uint8_t* __restrict__ x_scales,
-                                                             const uint8_t* __restrict__ w, const uint8_t* __restrict__ w_scales,
-                                                             const float* __restrict__ bias, void* __restrict__ out)
-{
-    extern __shared__ float sums[];                      // [wavefront][tile][lane][4]
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, waves = (int)blockDim.x >> 6;
+    constexpr bool kStored = std::is_same_v<X, Codes>;
+    extern __shared__ char lds[];                        // sums [wavefront][lane][4]; then x: codes [row][pieces * 64 + 16] (rows in other banks), scales [row][pieces * 4]
+    // (the wavefront's number in a scalar register: a matrix instruction in a branch that only masks lanes out would be executed)
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = (int)blockDim.x >> 6;
     const int r = lane & 15, kb = lane >> 4;
-    const uint32_t mt = fast_div(blockIdx.x, A.by_n), nt = blockIdx.x - mt * (uint32_t)A.n_tiles;
-    const int n0 = (int)nt * 16 * NT, m0 = (int)mt * 16 * MT;
-    floatx4 acc[NT][MT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int per = (A.pieces + waves - 1) / waves;
-    const int last = min(A.pieces, (wave + 1) * per);
+    const uint32_t block = fast_div(blockIdx.x, A.by_tiles), m_tile = blockIdx.x - block * (uint32_t)A.row_tiles;
+    const int n0 = (int)block * 16, m0 = (int)m_tile * kRows, rows = min(kRows, A.s.rows - m0);
     // rows past the end are read as the last one, and their results dropped
-    for (int piece = wave * per; piece < last; ++piece) {
-        uint4 a[NT], b[MT];
-        uint32_t sa[NT], sb[MT];
+    const long long n_row = (long long)min(n0 + r, A.s.out - 1) * A.pieces, m_row = (long long)(m0 + min(r, rows - 1)) * A.pieces;
+    const uint8_t* w_at = w + n_row * 64 + kb * 16;
+    const uint8_t* ws_at = w_scales + n_row * 4 + kb;
+    const uint8_t* x_at = static_cast<const uint8_t*>(x) + m_row * 64 + kb * 16;       // of codes
+    const uint8_t* xs_at = x_scales + m_row * 4 + kb;
+
+    uint4 a[kAhead], b[kStored ? kAhead : 1];
+    uint32_t sa[kAhead], sb[kStored ? kAhead : 1];
+    auto ask = [&](int first) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const long long row = (long long)min(n0 + i * 16 + r, A.s.out - 1) * A.pieces + piece;
-            a[i] = *reinterpret_cast<const uint4*>(w + row * 64 + kb * 16);
-            sa[i] = w_scales[row * 4 + kb];
+        for (int i = 0; i < kAhead; ++i) {
+            const int piece = min(first + i * waves, A.pieces - 1);      // past the end: the last one, which is not multiplied
+            a[i] = *reinterpret_cast<const uint4*>(w_at + piece * 64);
+            sa[i] = ws_at[piece * 4];
+            if constexpr (kStored) {
+                b[i] = *reinterpret_cast<const uint4*>(x_at + piece * 64);
+                sb[i] = xs_at[piece * 4];
+            }
         }
-#pragma unroll
-        for (int j = 0; j < MT; ++j) block_of<X>(A, x, x_scales, min(m0 + j * 16 + r, A.s.rows - 1), piece, kb, b[j], sb[j]);
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int j = 0; j < MT; ++j) acc[i][j] = multiply(a[i], b[j], acc[i][j], sa[i], sb[j]);
+    };
+    ask(wave);
+    const int pitch = A.pieces * 64 + 16;
+    char* const s_codes = lds + waves * 1024;
+    uint8_t* const s_scales = reinterpret_cast<uint8_t*>(s_codes) + rows * pitch;
+    if constexpr (!kStored) {
+        // a block's four lanes are neighbours; rows are multiples of 16 runs of eight values long
+        const int runs = A.pieces * 16;
+        for (int i = (int)threadIdx.x; i < (rows * runs + 63) / 64 * 64; i += (int)blockDim.x) {
+            const int row = (int)fast_div((uint32_t)i, A.by_lanes), run = i - row * runs;
+            Pack<X, 8> v;
+            uint32_t top = 0;
+            if (row < rows) {
+                v = load8(static_cast<const X*>(x) + (long long)(m0 + row) * A.s.x_row + run * 8, A.s.in - run * 8, A.whole_runs);
+                top = largest(v);
+            }
+            top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+            if (row < rows) {
+                const uint32_t byte = scale_byte(top);
+                *reinterpret_cast<uint32_t*>(s_codes + row * pitch + run * 4) = byte == kNanScale ? 0u : encode8(v, scale_of(byte));
+                if (run % 4 == 0) s_scales[i / 4] = (uint8_t)byte;
+            }
+        }
+        __syncthreads();
     }
+    const int x_row = min(r, rows - 1);
+    const char* s_code_at = s_codes + x_row * pitch + kb * 16;
+    const uint8_t* s_scale_at = s_scales + x_row * A.pieces * 4 + kb;
+    floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int first = wave; first < A.pieces; first += kAhead * waves) {
+        if (first != wave) ask(first);
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) *reinterpret_cast<floatx4*>(sums + ((wave * NT * MT + i * MT + j) * 64 + lane) * 4) = acc[i][j];
+        for (int i = 0; i < kAhead; ++i) {
+            const int piece = first + i * waves;
+            if (piece >= A.pieces) break;
+            if constexpr (kStored) acc = multiply(a[i], b[i], acc, sa[i], sb[i]);
+            else acc = multiply(a[i], *reinterpret_cast<const uint4*>(s_code_at + piece * 64), acc, sa[i], s_scale_at[piece * 4]);
+        }
+    }
+    float* sums = reinterpret_cast<float*>(lds);
+    *reinterpret_cast<floatx4*>(sums + (wave * 64 + lane) * 4) = acc;
     __syncthreads();
-    for (int t = (int)threadIdx.x; t < NT * MT * 256; t += (int)blockDim.x) {
-        const int nl = t % (NT * 16), ml = t / (NT * 16);
-        const int n = n0 + nl, m = m0 + ml;
-        if (n >= A.s.out || m >= A.s.rows) continue;
-        const int tile = (nl >> 4) * MT + (ml >> 4), at = (tile * 64 + ((nl & 15) >> 2) * 16 + (ml & 15)) * 4 + (nl & 3);
+    for (int t = (int)threadIdx.x; t < rows * 16; t += (int)blockDim.x) {
+        const int nl = t & 15, ml = t >> 4, n = n0 + nl;
+        if (n >= A.s.out) continue;
+        const int at = ((nl >> 2) * 16 + ml) * 4 + (nl & 3);
         float z = 0.0f;
-        for (int k = 0; k < waves; ++k) z += sums[k * NT * MT * 256 + at];
+        for (int k = 0; k < waves; ++k) z += sums[k * 256 + at];
         if (bias) z += bias[n];
-        store_as(out, (long long)m * A.s.out_row + n, A.s.out_type, activate_as(z, A.s.act));
+        store_as(out, (long long)(m0 + ml) * A.s.out_row + n, A.s.out_type, activate_as(z, A.s.act));
     }
 }
 
-// Rows up to which x is quantised where it is multiplied; above, once for all workgroups, in the workspace.
-constexpr int kDirectRows = 16;
-
-template <class X, int NT, int MT>
-hipError_t launch_direct(const LinearShape& s, const void* x, const uint8_t* x_scales, const uint8_t* w, const uint8_t* w_scales, const float* bias,
-                         void* out, hipStream_t stream)
+template <class X>
+hipError_t launch_rows(const LinearShape& s, const void* x, const uint8_t* x_scales, const uint8_t* w, const uint8_t* w_scales, const float* bias,
+                       void* out, hipStream_t stream)
 {
-    Args A{s, (int)mxfp4_pieces(s.in), (s.out + 16 * NT - 1) / (16 * NT), (s.rows + 16 * MT - 1) / (16 * MT), false, {}};
-    A.by_n = make_fast_div((uint32_t)A.n_tiles);
-    if (s.x_type != kMxfp4)
-        A.whole_runs = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (s.rows == 1 || s.x_row * (long long)element_bytes(s.x_type) % 16 == 0);
-    const int waves = std::min(NT * MT > 1 ? 4 : 16, A.pieces);
-    hipLaunchKernelGGL((linear_direct_kernel<X, NT, MT>), dim3((unsigned)((long long)A.n_tiles * A.m_tiles)), dim3((unsigned)waves * 64),
-                       (size_t)waves * NT * MT * 1024, stream, A, x, x_scales, w, w_scales, bias, out);
+    Args A{s, (int)mxfp4_pieces(s.in), (s.rows + kRows - 1) / kRows, false, {}, {}};
+    A.by_tiles = make_fast_div((uint32_t)A.row_tiles);
+    A.by_lanes = make_fast_div((uint32_t)A.pieces * 16);
+    size_t x_bytes = 0;
+    if constexpr (!std::is_same_v<X, Codes>) {
+        A.whole_runs = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (s.rows == 1 || s.x_row * (long long)sizeof(X) % 16 == 0);
+        x_bytes = (size_t)std::min(s.rows, kRows) * (A.pieces * 68 + 16);
+    }
+    const int waves = std::min(16, A.pieces);
+    const size_t lds = (size_t)waves * 1024 + x_bytes;
+    static std::atomic<uint64_t> allowed{0};
+    if (lds > 64 * 1024)
+        if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(linear_rows_kernel<X>), allowed); e != hipSuccess) return e;
+    hipLaunchKernelGGL((linear_rows_kernel<X>), dim3((unsigned)((long long)((s.out + 15) / 16) * A.row_tiles)), dim3((unsigned)waves * 64), lds, stream,
+                       A, x, x_scales, w, w_scales, bias, out);
     return hipGetLastError();
+}
+
+// Whether x is quantised where it is multiplied.
+bool in_one_launch(const LinearShape& s)
+{
+    return s.x_type != kMxfp4 && s.rows <= kRows && s.rows * (mxfp4_pieces(s.in) * 68 + 16) <= kRowsLds;
 }
 
 }  // namespace
@@ -129,7 +153,7 @@ bool linear_fits(const LinearShape& s)
 
 namespace {
 
-// The workspace: codes and scales of x where it is quantised beforehand, then the slices' sums.
+// The workspace: codes and scales of x where it is quantised in a launch of its own, then the slices' sums.
 struct Room {
     bool quantised_here;
     TilePlan plan;
@@ -138,7 +162,7 @@ struct Room {
 Room room_of(const LinearShape& s)
 {
     Room r{};
-    r.quantised_here = s.x_type != kMxfp4 && s.rows > kDirectRows;
+    r.quantised_here = s.x_type != kMxfp4 && !in_one_launch(s);
     r.plan = tile_plan(s);
     const size_t blocks = r.quantised_here ? (size_t)s.rows * (size_t)mxfp4_pieces(s.in) * 4 : 0;
     r.scales_at = blocks * 16;
@@ -158,7 +182,7 @@ hipError_t launch_linear(const LinearShape& s, const void* x, const uint8_t* x_s
     uint8_t* work = static_cast<uint8_t*>(workspace);
     if (s.x_type != kMxfp4 && !room.quantised_here) {
         hipError_t e = hipSuccess;
-        with_type(s.x_type, [&](auto t) { e = launch_direct<decltype(t), 1, 1>(s, x, nullptr, w, w_scales, bias, out, stream); });
+        with_type(s.x_type, [&](auto t) { e = launch_rows<decltype(t)>(s, x, nullptr, w, w_scales, bias, out, stream); });
         return e;
     }
     if (room.quantised_here) {
@@ -169,7 +193,7 @@ hipError_t launch_linear(const LinearShape& s, const void* x, const uint8_t* x_s
     }
     if (room.plan.shape >= 0)
         return launch_tiles(s, room.plan, x, x_scales, w, w_scales, bias, out, reinterpret_cast<float*>(work + room.sums_at), stream);
-    return launch_direct<Codes, 1, 1>(s, x, x_scales, w, w_scales, bias, out, stream);
+    return launch_rows<Codes>(s, x, x_scales, w, w_scales, bias, out, stream);
 }
 
 }  // namespace patdnn

@@ -13,9 +13,10 @@ enum { kActNone = 0, kActRelu = 1, kActSilu = 2 };       // the PATDNN_ACT_...
 
 inline size_t element_bytes(int type) { return type == kF32 ? 4 : 2; }
 
-// V elements side by side, moved with one access.
+// V elements side by side, moved with one access, which needs no more alignment than the elements have: gfx950's vector memory
+// instructions take any address.
 template <class T, int V>
-struct alignas(sizeof(T) * V) Pack {
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
     T v[V];
 };
 

@@ -25,7 +25,6 @@ constexpr int kRowsLds = 128 * 1024;                     // most bytes of x in L
 struct Args {
     LinearShape s;
     int pieces, row_tiles;                               // of 128 along k; of kRows rows of x
-    bool whole_runs;                                     // rows of x in runs of 16 bytes
     FastDiv by_tiles, by_lanes;                          // row_tiles; runs of eight values in a row of x
 };
 
@@ -74,7 +73,7 @@ __global__ __launch_bounds__(1024) void linear_rows_kernel(Args A, const void* _
             Pack<X, 8> v;
             uint32_t top = 0;
             if (row < rows) {
-                v = load8(static_cast<const X*>(x) + (long long)(m0 + row) * A.s.x_row + run * 8, A.s.in - run * 8, A.whole_runs);
+                v = load8(static_cast<const X*>(x) + (long long)(m0 + row) * A.s.x_row + run * 8, A.s.in - run * 8);
                 top = largest(v);
             }
             top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
@@ -119,14 +118,11 @@ template <class X>
 hipError_t launch_rows(const LinearShape& s, const void* x, const uint8_t* x_scales, const uint8_t* w, const uint8_t* w_scales, const float* bias,
                        void* out, hipStream_t stream)
 {
-    Args A{s, (int)mxfp4_pieces(s.in), (s.rows + kRows - 1) / kRows, false, {}, {}};
+    Args A{s, (int)mxfp4_pieces(s.in), (s.rows + kRows - 1) / kRows, {}, {}};
     A.by_tiles = make_fast_div((uint32_t)A.row_tiles);
     A.by_lanes = make_fast_div((uint32_t)A.pieces * 16);
     size_t x_bytes = 0;
-    if constexpr (!std::is_same_v<X, Codes>) {
-        A.whole_runs = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (s.rows == 1 || s.x_row * (long long)sizeof(X) % 16 == 0);
-        x_bytes = (size_t)std::min(s.rows, kRows) * (A.pieces * 68 + 16);
-    }
+    if constexpr (!std::is_same_v<X, Codes>) x_bytes = (size_t)std::min(s.rows, kRows) * (A.pieces * 68 + 16);
     const int waves = std::min(16, A.pieces);
     const size_t lds = (size_t)waves * 1024 + x_bytes;
     static std::atomic<uint64_t> allowed{0};

@@ -22,7 +22,6 @@ struct Args {
     int pieces;                                          // stages along k
     int tiles_n, tiles_m, slices, slice_pieces;          // slices of k, whole groups of four stages each
     bool wide_scales;                                    // rows of scales in whole aligned runs of 16 bytes
-    bool runs;                                           // output rows in runs of 16 bytes
     FastDiv by_tiles, by_band, by_last;                  // tiles of a slice, of a band, rows of tiles of the last band
 };
 constexpr int kBand = 8;                                 // rows of tiles that are taken side by side
@@ -217,27 +216,10 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tiles_kernel(Args A, cons
                 if (A.slices == 1) z[i] = activate_as(z[i] + add[i], A.s.act);
             }
             const long long at = m * out_row + n;
-            if (A.runs && n + 16 <= A.s.out) {
-                if (type == kF32) {
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) store_pack<float, 4>(static_cast<float*>(to) + at + i, Pack<float, 4>{{z[i], z[i + 1], z[i + 2], z[i + 3]}});
-                } else if (type == kF16) {
-#pragma unroll
-                    for (int i = 0; i < 16; i += 8) {
-                        Pack<_Float16, 8> p;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) p.v[e] = from_float<_Float16>(z[i + e]);
-                        store_pack<_Float16, 8>(static_cast<_Float16*>(to) + at + i, p);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; i += 8) {
-                        Pack<__bf16, 8> p;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) p.v[e] = from_float<__bf16>(z[i + e]);
-                        store_pack<__bf16, 8>(static_cast<__bf16*>(to) + at + i, p);
-                    }
-                }
+            if (n + 16 <= A.s.out) {
+                if (type == kF32) store_sixteen<float>(to, at, z);
+                else if (type == kF16) store_sixteen<_Float16>(to, at, z);
+                else store_sixteen<__bf16>(to, at, z);
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
@@ -316,8 +298,6 @@ hipError_t launch_tiles(const LinearShape& s, const TilePlan& p, const void* x, 
     A.slice_pieces = (((A.pieces + 3) / 4 + p.slices - 1) / p.slices) * 4;
     A.slices = (A.pieces + A.slice_pieces - 1) / A.slice_pieces;
     A.wide_scales = A.pieces % 4 == 0 && (reinterpret_cast<uintptr_t>(x_scales) | reinterpret_cast<uintptr_t>(w_scales)) % 16 == 0;
-    A.runs = A.slices > 1 ? s.out % 4 == 0
-                          : reinterpret_cast<uintptr_t>(out) % 16 == 0 && s.out_row * (long long)element_bytes(s.out_type) % 16 == 0;
     hipError_t e = p.shape == 0   ? launch_shape<256, 256, 2, 4>(A, x, x_scales, w, w_scales, bias, out, partial, stream)
                    : p.shape == 1 ? launch_shape<128, 128, 2, 2>(A, x, x_scales, w, w_scales, bias, out, partial, stream)
                                   : launch_shape<64, 64, 1, 4>(A, x, x_scales, w, w_scales, bias, out, partial, stream);

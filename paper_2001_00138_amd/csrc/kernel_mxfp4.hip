@@ -45,7 +45,7 @@ __device__ __forceinline__ bool place_of(const Mxfp4Shape& s, const Spread& p, i
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads) void quantize_kernel(Mxfp4Shape s, Spread p, bool whole_runs, const T* __restrict__ x,
+__global__ __launch_bounds__(kThreads) void quantize_kernel(Mxfp4Shape s, Spread p, const T* __restrict__ x,
                                                             uint32_t* __restrict__ codes, uint8_t* __restrict__ scales)
 {
     int row, run;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(Mxfp4Shape s, Spread
     Pack<T, 8> a;
     uint32_t top = 0;
     if (mine) {
-        a = load8(x + (long long)row * s.row + run * 8, s.cols - run * 8, whole_runs);
+        a = load8(x + (long long)row * s.row + run * 8, s.cols - run * 8);
         top = largest(a);
     }
     // four lanes of a block are neighbours in a wavefront: runs of a row and workgroup start at multiples of 16
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(Mxfp4Shape s, Spread
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads) void dequantize_kernel(Mxfp4Shape s, Spread p, bool whole_runs, const uint32_t* __restrict__ codes,
+__global__ __launch_bounds__(kThreads) void dequantize_kernel(Mxfp4Shape s, Spread p, const uint32_t* __restrict__ codes,
                                                               const uint8_t* __restrict__ scales, T* __restrict__ out)
 {
     int row, run;
@@ -81,26 +81,13 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(Mxfp4Shape s, Spre
     Pack<T, 8> r;
 #pragma unroll
     for (int i = 0; i < 8; ++i) r.v[i] = from_float<T>(byte == kNanScale ? __builtin_nanf("") : v[i / 2][i % 2]);
-    if (whole_runs && left >= 8) {
-        constexpr int kRun = 16 / (int)sizeof(T);
-#pragma unroll
-        for (int i = 0; i < 8; i += kRun) {
-            Pack<T, kRun> part;
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) part.v[j] = r.v[i + j];
-            store_pack<T, kRun>(to + i, part);
-        }
+    if (left >= 8) {
+        store_pack<T, 8>(to, r);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < left) to[i] = r.v[i];
     }
-}
-
-// Whether every run of eight values starts at a multiple of 16 bytes.
-bool aligned_runs(const Mxfp4Shape& s, const void* p)
-{
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (s.rows == 1 || s.row * (long long)element_bytes(s.type) % 16 == 0);
 }
 
 }  // namespace
@@ -111,8 +98,7 @@ hipError_t launch_mxfp4_quantize(const Mxfp4Shape& s, const void* x, uint8_t* co
 {
     with_type(s.type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL((quantize_kernel<T>), dim3((unsigned)blocks_of(s)), dim3(kThreads), 0, stream, s, spread_of(s), aligned_runs(s, x),
-                           static_cast<const T*>(x), reinterpret_cast<uint32_t*>(codes), scales);
+        hipLaunchKernelGGL((quantize_kernel<T>), dim3((unsigned)blocks_of(s)), dim3(kThreads), 0, stream, s, spread_of(s), static_cast<const T*>(x), reinterpret_cast<uint32_t*>(codes), scales);
     });
     return hipGetLastError();
 }
@@ -121,8 +107,7 @@ hipError_t launch_mxfp4_dequantize(const Mxfp4Shape& s, const uint8_t* codes, co
 {
     with_type(s.type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL((dequantize_kernel<T>), dim3((unsigned)blocks_of(s)), dim3(kThreads), 0, stream, s, spread_of(s), aligned_runs(s, out),
-                           reinterpret_cast<const uint32_t*>(codes), scales, static_cast<T*>(out));
+        hipLaunchKernelGGL((dequantize_kernel<T>), dim3((unsigned)blocks_of(s)), dim3(kThreads), 0, stream, s, spread_of(s), reinterpret_cast<const uint32_t*>(codes), scales, static_cast<T*>(out));
     });
     return hipGetLastError();
 }

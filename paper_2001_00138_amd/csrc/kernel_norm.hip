@@ -287,9 +287,9 @@ struct Held {
     FastDiv by_chunks, by_tx, by_cpg, by_entries, by_chunk;
 };
 
-// Most runs that a lane holds: 64 registers of them (32 of one or two bytes).
+// Most runs that a lane holds, so that nothing spills: of 16 bytes, of eight, of fewer.
 template <class T, int V>
-constexpr int held_runs() { return V * sizeof(T) >= 16 ? 16 : 32; }
+constexpr int held_runs() { return V * sizeof(T) >= 16 ? 16 : V * sizeof(T) == 8 ? 24 : 32; }
 
 __device__ __forceinline__ uint32_t held_block(uint32_t total)
 {
@@ -307,9 +307,12 @@ struct Kept {
     __device__ __forceinline__ void load(const T* p)
     {
         if constexpr (V * sizeof(T) >= 4) {
-            const Pack<uint32_t, kWords> a = load_pack<uint32_t, kWords>(reinterpret_cast<const uint32_t*>(p));
+            struct __attribute__((packed, aligned(sizeof(T)))) Words {
+                uint32_t w[kWords];
+            };
+            const Words a = *reinterpret_cast<const Words*>(p);
 #pragma unroll
-            for (int i = 0; i < kWords; ++i) w[i] = a.v[i];
+            for (int i = 0; i < kWords; ++i) w[i] = a.w[i];
         } else {
             w[0] = *reinterpret_cast<const unsigned short*>(p);
         }
@@ -998,7 +1001,7 @@ Geometry geometry_of(const NormShape& s)
         G.per_group = (G.cpg + kChunk - 1) / kChunk;
         G.chunks = s.groups * G.per_group;
     } else {
-        // whole groups, and a multiple of eight channels if there is one, so that the lanes' runs stay aligned
+        // whole groups, and a multiple of eight channels if there is one, so that lanes have whole runs
         int unit = G.cpg;
         while (unit % 8 && unit + G.cpg <= kChunk) unit += G.cpg;
         if (unit % 8) unit = G.cpg;
@@ -1016,21 +1019,16 @@ Geometry geometry_of(const NormShape& s)
     return G;
 }
 
-// Elements that a lane moves with one access: as many as everything is aligned to, up to 16 bytes of them.
-int aligned_run(const NormShape& s, const void* const* pointers, const long long* strides, int count)
+// Elements that a lane moves with one access: up to 16 bytes of them, and the channels (of a chunk, of a part of a group) a multiple.
+int run_of(const NormShape& s)
 {
-    const int bytes = (int)element_bytes(s.type);
-    uint64_t all = (uint64_t)s.c;
-    for (int i = 0; i < count; ++i) all |= reinterpret_cast<uintptr_t>(pointers[i]) / bytes;
-    for (int i = 0; i < 2 * count; ++i) all |= (uint64_t)strides[i];
-    int v = 16 / bytes;
-    while (all % (uint64_t)v) v /= 2;
+    int v = 16 / (int)element_bytes(s.type);
+    while (s.c % v) v /= 2;
     return v;
 }
-// The same where chunks and slabs are taken.
-int run_of(const Geometry& G, const void* const* pointers, const long long* strides, int count)
+int run_of(const Geometry& G)
 {
-    int v = aligned_run(G.s, pointers, strides, count);
+    int v = run_of(G.s);
     while ((G.chunks > 1 && G.chunk % v) || (G.per_group > 1 && G.cpg % v)) v /= 2;
     return v;
 }
@@ -1164,9 +1162,7 @@ size_t norm_workspace_floats(const NormShape& s, bool backward)
 hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd,
                        float* workspace, hipStream_t stream)
 {
-    const void* pointers[] = {x, y};
-    const long long strides[] = {s.x_image, s.x_pixel, s.y_image, s.y_pixel};
-    for (int v = aligned_run(s, pointers, strides, 2); v > 0; v /= 2) {
+    for (int v = run_of(s); v > 0; v /= 2) {
         hipError_t e = hipErrorNotReady;
         with_type(s.type, [&](auto t) {
             using T = decltype(t);
@@ -1197,7 +1193,7 @@ hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, co
         if (e != hipErrorNotReady) return e;
     }
     Geometry G = geometry_of(s);
-    const int v = run_of(G, pointers, strides, 2);
+    const int v = run_of(G);
     finish(G, v);
     const dim3 grid((unsigned)(s.n * G.chunks * G.slabs));
     with_type(s.type, [&](auto t) {
@@ -1225,8 +1221,6 @@ hipError_t launch_norm_backward(const NormShape& s, const void* dy, const void* 
         if (dbeta && (e = launch_fill_zero(dbeta, (size_t)s.c, stream)) != hipSuccess) return e;
         return hipSuccess;
     }
-    const void* pointers[] = {x, dx, dy};
-    const long long strides[] = {s.x_image, s.x_pixel, s.y_image, s.y_pixel, s.dy_image, s.dy_pixel};
     // Held where lanes have whole runs of 16 bytes, and sums fold or pixels are few: the other way to add columns up costs more than reading
     // twice (8 x 56x56x64 in groups of two, fp32: 23 us and 15).
     e = hipErrorNotReady;
@@ -1235,7 +1229,7 @@ hipError_t launch_norm_backward(const NormShape& s, const void* dy, const void* 
         constexpr int V = 16 / (int)sizeof(T);
         // two-byte values: eight runs take as long as reading twice where thirteen do not fit the registers any more
         constexpr int kMost = sizeof(T) == 4 ? 13 : 8;
-        if (aligned_run(s, pointers, strides, 3) != V) return;
+        if (run_of(s) != V) return;
         Held H;
         int threads, runs;
         const int fewer = s.c / s.groups % V == 0 ? kMost : sizeof(T) == 4 ? 8 : 4;      // more constants a lane: fewer runs
@@ -1264,7 +1258,7 @@ hipError_t launch_norm_backward(const NormShape& s, const void* dy, const void* 
     }
     if (e != hipErrorNotReady) return e;
     Geometry G = geometry_of(s);
-    const int v = run_of(G, pointers, strides, 3);
+    const int v = run_of(G);
     finish(G, v);
     const unsigned blocks = (unsigned)(s.n * G.chunks * G.slabs);
     const int params = dgamma || dbeta ? param_blocks_of(s) : 0;

@@ -18,6 +18,20 @@ __device__ __forceinline__ float activate_as(float z, int act)
     return act == kActRelu ? activate<kActRelu>(z) : act == kActSilu ? activate<kActSilu>(z) : z;
 }
 
+// Sixteen neighbouring results.
+template <class T>
+__device__ __forceinline__ void store_sixteen(void* out, long long at, const float (&z)[16])
+{
+    constexpr int kRun = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 16; i += kRun) {
+        Pack<T, kRun> p;
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) p.v[e] = from_float<T>(z[i + e]);
+        store_pack<T, kRun>(static_cast<T*>(out) + at + i, p);
+    }
+}
+
 // The tiled kernel (kernel_linear_tiles.hip), codes times codes.  Which shape it takes, and along how many slices of k.
 struct TilePlan {
     int shape = -1;                                      // -1: not this kernel

@@ -84,17 +84,11 @@ __device__ __forceinline__ uint32_t encode8(const Pack<__bf16, 8>& a, float scal
 
 // Eight values from p on, those from `left` on (of the row) zero.
 template <class T>
-__device__ __forceinline__ Pack<T, 8> load8(const T* p, int left, bool whole_runs)
+__device__ __forceinline__ Pack<T, 8> load8(const T* p, int left)
 {
     Pack<T, 8> a;
-    if (whole_runs && left >= 8) {
-        constexpr int kRun = 16 / (int)sizeof(T);
-#pragma unroll
-        for (int i = 0; i < 8; i += kRun) {
-            const Pack<T, kRun> b = load_pack<T, kRun>(p + i);
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) a.v[i + j] = b.v[j];
-        }
+    if (left >= 8) {
+        a = load_pack<T, 8>(p);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) a.v[i] = i < left ? p[i] : T(0.0f);

@@ -158,7 +158,8 @@ struct Room {
 Room room_of(const LinearShape& s)
 {
     Room r{};
-    r.quantised_here = s.x_type != kMxfp4 && !in_one_launch(s);
+    r.quantised_here = s.x_type != kMxfp4 && !in_one_launch(s) && !short_fits(s);
+    if (short_fits(s)) return r;
     r.plan = tile_plan(s);
     const size_t blocks = r.quantised_here ? (size_t)s.rows * (size_t)mxfp4_pieces(s.in) * 4 : 0;
     r.scales_at = blocks * 16;
@@ -174,6 +175,7 @@ size_t linear_workspace_bytes(const LinearShape& s) { return room_of(s).bytes; }
 hipError_t launch_linear(const LinearShape& s, const void* x, const uint8_t* x_scales, const uint8_t* w, const uint8_t* w_scales, const float* bias,
                          void* out, void* workspace, hipStream_t stream)
 {
+    if (short_fits(s)) return launch_short(s, x, x_scales, w, w_scales, bias, out, stream);
     const Room room = room_of(s);
     uint8_t* work = static_cast<uint8_t*>(workspace);
     if (s.x_type != kMxfp4 && !room.quantised_here) {

@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tiles_kernel(Args A, cons
     }
 
     // A lane's results: row m0 + ... + r of x, for each four tiles sixteen neighbouring outputs.
-    const int type = A.slices > 1 ? kF32 : A.s.out_type;
+    const int type = A.slices > 1 ? kF32 : A.s.out_type, act = A.slices > 1 ? kActNone : A.s.act;
     void* to = A.slices > 1 ? static_cast<void*>(partial + (long long)slice * A.s.rows * A.s.out) : out;
     const long long out_row = A.slices > 1 ? A.s.out : A.s.out_row;
 #pragma unroll
@@ -211,20 +211,9 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tiles_kernel(Args A, cons
             if (m >= A.s.rows || n >= A.s.out) continue;
             float z[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                z[i] = acc[g * 4 + i / 4][j][i % 4];
-                if (A.slices == 1) z[i] = activate_as(z[i] + add[i], A.s.act);
-            }
-            const long long at = m * out_row + n;
-            if (n + 16 <= A.s.out) {
-                if (type == kF32) store_sixteen<float>(to, at, z);
-                else if (type == kF16) store_sixteen<_Float16>(to, at, z);
-                else store_sixteen<__bf16>(to, at, z);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (n + i < A.s.out) store_as(to, at + i, type, z[i]);
-            }
+            for (int i = 0; i < 16; ++i) z[i] = acc[g * 4 + i / 4][j][i % 4] + add[i];
+            finish_sixteen(z, act);
+            store_results(to, m * out_row + n, type, A.s.out - n, z);
         }
     }
 }

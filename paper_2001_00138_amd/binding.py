@@ -549,6 +549,8 @@ def _channels_last_layout(t, name: str):
     if dims < 3:
         raise ValueError(f"{name} must be [n, ..., channels]")
     c = shape[-1]
+    if dims == 4 and strides[-1] == 1 and strides[1] == strides[2] * shape[2]:       # most calls'
+        return shape[0], shape[1] * shape[2], c, strides[0], strides[2]
     if c > 1 and strides[-1] != 1 and t.numel():
         raise ValueError(f"the channels of {name} must be adjacent")
     pixel, pixels = strides[-2], shape[-2]
@@ -592,13 +594,14 @@ def patdnn_channels_first(x, out=None, *, dtype=None, stream=None):
 
 
 def _norm_workspace(desc, backward: int, workspace, like, stream):
+    """-> (tensor, its floats)"""
     torch = _torch()
-    floats = lib().patdnn_group_norm_workspace_floats(ctypes.byref(desc), backward)
     if workspace is None:
-        workspace = _new((floats,), torch.float32, like, stream)
-    elif workspace.dtype != torch.float32:
+        floats = lib().patdnn_group_norm_workspace_floats(desc, backward)
+        return _new((floats,), torch.float32, like, stream), floats
+    if workspace.dtype != torch.float32:
         raise ValueError("workspace must be a float32 tensor")
-    return workspace
+    return workspace, workspace.numel()
 
 
 def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e-5, act="none", mean=None, rstd=None, workspace=None,
@@ -616,11 +619,11 @@ def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e
         mean = _new((n, groups), torch.float32, x, stream)
     if rstd is None:
         rstd = _new((n, groups), torch.float32, x, stream)
-    desc = NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), eps, x_image, x_pixel, y_image, y_pixel, 0, 0)
-    workspace = _norm_workspace(desc, 0, workspace, x, stream)
-    _check(lib().patdnn_group_norm(ctypes.byref(desc), x.data_ptr(), _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"),
+    desc = ctypes.byref(NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), eps, x_image, x_pixel, y_image, y_pixel, 0, 0))
+    workspace, floats = _norm_workspace(desc, 0, workspace, x, stream)
+    _check(lib().patdnn_group_norm(desc, x.data_ptr(), _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"),
                                    out.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
-                                   _devptr(workspace), workspace.numel(), _stream_ptr(stream)))
+                                   _devptr(workspace), floats, _stream_ptr(stream)))
     return out, mean, rstd
 
 
@@ -641,12 +644,12 @@ def patdnn_group_norm_backward(dy, x, mean, rstd, groups: int, gamma=None, beta=
         dgamma = _new((c,), torch.float32, x, stream)
     if dbeta is None:
         dbeta = _new((c,), torch.float32, x, stream)
-    desc = NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), 0.0, x_image, x_pixel, y_image, y_pixel, dy_image, dy_pixel)
-    workspace = _norm_workspace(desc, 1, workspace, x, stream)
+    desc = ctypes.byref(NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), 0.0, x_image, x_pixel, y_image, y_pixel, dy_image, dy_pixel))
+    workspace, floats = _norm_workspace(desc, 1, workspace, x, stream)
     _check(lib().patdnn_group_norm_backward(
-        ctypes.byref(desc), dy.data_ptr(), x.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
+        desc, dy.data_ptr(), x.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
         _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"), out.data_ptr(), _float_vector(dgamma, c, "dgamma"),
-        _float_vector(dbeta, c, "dbeta"), _devptr(workspace), workspace.numel(), _stream_ptr(stream)))
+        _float_vector(dbeta, c, "dbeta"), _devptr(workspace), floats, _stream_ptr(stream)))
     return out, dgamma, dbeta
 
 

@@ -133,10 +133,15 @@ hipError_t launch_rows(const LinearShape& s, const void* x, const uint8_t* x_sca
     return hipGetLastError();
 }
 
-// Whether x is quantised where it is multiplied.
+// Whether x is quantised where it is multiplied.  16 rows: as long as their codes fit LDS.  Up to 63 (then there is the kernel of short rows): every
+// workgroup quantises its 16 rows, which pays for itself while rows are short and a CU has at most one workgroup (48 x 1024 -> 1000 fp16: 8 us and 11 through tiles;
+// -> 4096 17 and 11; 32 x 4096 -> 1000 14 and 14).
 bool in_one_launch(const LinearShape& s)
 {
-    return s.x_type != kMxfp4 && s.rows <= kRows && s.rows * (mxfp4_pieces(s.in) * 68 + 16) <= kRowsLds;
+    if (s.x_type == kMxfp4) return false;
+    const long long pieces = mxfp4_pieces(s.in);
+    if (s.rows <= kRows) return s.rows * (pieces * 68 + 16) <= kRowsLds;
+    return s.rows < 64 && (pieces <= 4 || (pieces <= 16 && (long long)((s.rows + kRows - 1) / kRows) * ((s.out + 15) / 16) <= 256));
 }
 
 }  // namespace
@@ -158,10 +163,11 @@ struct Room {
 Room room_of(const LinearShape& s)
 {
     Room r{};
-    r.quantised_here = s.x_type != kMxfp4 && !in_one_launch(s) && !short_fits(s);
     if (short_fits(s)) return r;
+    r.quantised_here = s.x_type != kMxfp4 && !in_one_launch(s);
     r.plan = tile_plan(s);
-    const size_t blocks = r.quantised_here ? (size_t)s.rows * (size_t)mxfp4_pieces(s.in) * 4 : 0;
+    // (more than kRows rows: room for the codes whichever way the call takes, so that a change of that choice is no caller's concern)
+    const size_t blocks = r.quantised_here || (s.x_type != kMxfp4 && s.rows > kRows) ? (size_t)s.rows * (size_t)mxfp4_pieces(s.in) * 4 : 0;
     r.scales_at = blocks * 16;
     r.sums_at = (r.scales_at + blocks + 15) / 16 * 16;
     r.bytes = r.sums_at + tile_workspace_bytes(s, r.plan);

@@ -659,11 +659,11 @@ template <int R>
 constexpr int held_in_lds() { return R > 8 ? 9 : 0; }
 
 // The backward pass of what norm_held_kernel does.  x and dy are both held: R runs of either, of dy the first held_in_lds<R>() in LDS.
-// sums: [image][2][channel], dz and dz xh over the image's pixels.
+// sums_a, sums_b: dz and dz xh over an image's pixels, per channel, images 2 * channels floats apart.
 template <class T, int V, int R, bool ONE>
 __global__ __launch_bounds__(1024) void norm_back_held_kernel(Held G, const T* __restrict__ dy, const T* __restrict__ x, const float* __restrict__ mean_in,
                                                               const float* __restrict__ rstd_in, const float* __restrict__ gamma,
-                                                              const float* __restrict__ beta, T* __restrict__ dx, float* __restrict__ sums)
+                                                              const float* __restrict__ beta, T* __restrict__ dx, float* __restrict__ sums_a, float* __restrict__ sums_b)
 {
     constexpr int kInLds = held_in_lds<R>(), M = ONE ? 1 : V;
     using Run = Kept<T, V>;
@@ -748,7 +748,8 @@ __global__ __launch_bounds__(1024) void norm_back_held_kernel(Held G, const T* _
 #pragma unroll
     for (int i = 0; i < V; ++i) b[i] *= rstd[ONE ? 0 : i];
 
-    float* const to = sums + (long long)n * 2 * G.s.c + c0;
+    float* const to_a = sums_a + (long long)n * 2 * G.s.c + c0;
+    float* const to_b = sums_b + (long long)n * 2 * G.s.c + c0;
     float shift[M], slope[M];                            // of Channel's comment
     if (ONE && G.folded) {
         // over the rows of lanes of a wavefront by exchange, then the wavefronts; a group's sums likewise
@@ -788,7 +789,7 @@ __global__ __launch_bounds__(1024) void norm_back_held_kernel(Held G, const T* _
             const int half = i >= G.chunk, at = i - half * G.chunk;
             float v = 0.0f;
             for (int k = 0; k < waves; ++k) v += s_channel[(k * 2 + half) * G.chunk + at];
-            if (at < width) to[half * G.s.c + at] = v;
+            if (at < width) (half ? to_b : to_a)[at] = v;
         }
         shift[0] = rstd[0] * (ag * G.inv_m);
         slope[0] = rstd[0] * rstd[0] * (bg * G.inv_m);
@@ -823,8 +824,8 @@ __global__ __launch_bounds__(1024) void norm_back_held_kernel(Held G, const T* _
                 pa += s_part[(k * 2) * pitch + i];
                 pb += s_part[(k * 2 + 1) * pitch + i];
             }
-            to[i] = pa;
-            to[G.s.c + i] = pb;
+            to_a[i] = pa;
+            to_b[i] = pb;
             const float weight = gamma ? gamma[c0 + i] : 1.0f;
             s_a[i] = weight * pa;
             s_b[i] = weight * pb;
@@ -1131,14 +1132,15 @@ size_t held_back_lds(const Held& H, int v, int threads, int in_lds, size_t run_b
 
 template <class T, int V, int R, bool ONE>
 hipError_t launch_held_back(const Held& H, int threads, const void* dy, const void* x, const float* mean, const float* rstd, const float* gamma,
-                            const float* beta, void* dx, float* sums, hipStream_t stream)
+                            const float* beta, void* dx, float* sums_a, float* sums_b, hipStream_t stream)
 {
     static std::atomic<uint64_t> allowed{0};
     const size_t lds = held_back_lds(H, V, threads, held_in_lds<R>(), sizeof(Kept<T, V>));
     if (lds > 64 * 1024)
         if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(norm_back_held_kernel<T, V, R, ONE>), allowed); e != hipSuccess) return e;
     hipLaunchKernelGGL((norm_back_held_kernel<T, V, R, ONE>), dim3((unsigned)(H.s.n * H.chunks)), dim3((unsigned)threads), lds, stream, H,
-                       static_cast<const T*>(dy), static_cast<const T*>(x), mean, rstd, gamma, beta, static_cast<T*>(dx), sums);
+                       static_cast<const T*>(dy), static_cast<const T*>(x), mean, rstd, gamma, beta, static_cast<T*>(dx),
+                       sums_a, sums_b);
     return hipGetLastError();
 }
 
@@ -1224,6 +1226,9 @@ hipError_t launch_norm_backward(const NormShape& s, const void* dy, const void* 
     // Held where lanes have whole runs of 16 bytes, and sums fold or pixels are few: the other way to add columns up costs more than reading
     // twice (8 x 56x56x64 in groups of two, fp32: 23 us and 15).
     e = hipErrorNotReady;
+    // one image: its sums are dbeta and dgamma
+    float* const sums_a = s.n == 1 && dbeta ? dbeta : workspace;
+    float* const sums_b = s.n == 1 && dgamma ? dgamma : workspace + s.c;
     with_type(s.type, [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
@@ -1242,17 +1247,17 @@ hipError_t launch_norm_backward(const NormShape& s, const void* dy, const void* 
             constexpr int R = decltype(r)::value;
             if constexpr (R <= (sizeof(T) == 4 ? 8 : 4))
                 if (H.cpg % V) {
-                    e = launch_held_back<T, V, R, false>(H, threads, dy, x, mean, rstd, gamma, beta, dx, workspace, stream);
+                    e = launch_held_back<T, V, R, false>(H, threads, dy, x, mean, rstd, gamma, beta, dx, sums_a, sums_b, stream);
                     return;
                 }
-            e = launch_held_back<T, V, R, true>(H, threads, dy, x, mean, rstd, gamma, beta, dx, workspace, stream);
+            e = launch_held_back<T, V, R, true>(H, threads, dy, x, mean, rstd, gamma, beta, dx, sums_a, sums_b, stream);
         };
         if (runs <= 2) with_runs(Const<2>{});
         else if (runs <= 4) with_runs(Const<4>{});
         else if (runs <= 8) with_runs(Const<8>{});
         else with_runs(Const<kMost>{});
     });
-    if (e == hipSuccess && (dgamma || dbeta)) {
+    if (e == hipSuccess && s.n > 1 && (dgamma || dbeta)) {
         hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)param_blocks_of(s)), dim3(kThreads), 0, stream, s.c, s.n, workspace, dgamma, dbeta);
         e = hipGetLastError();
     }

@@ -1,0 +1,80 @@
+"""The operators' kernels that only larger sizes reach, against the oracle in 64 bits: group norm in one launch and in two, with every run length
+and several chunks of a group; linear layers through each shape of tiles, with short rows, in slices.  Tolerances as in test_gpu_norm.py and
+test_gpu_mxfp4.py."""
+
+import pytest
+
+import test_gpu_mxfp4 as mx
+import test_gpu_norm as norm
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch
+
+
+# one launch: lanes with one run and with many, 16-byte runs and shorter ones, groups that are lanes' powers of two and not; many images;
+# two launches: narrow groups of many pixels, groups of more channels than a chunk, in parts; last slabs and last chunks that are short
+SHAPES = [(1, 3136, 64, 8), (1, 3136, 128, 32), (2, 4096, 32, 4), (300, 196, 64, 2), (600, 49, 32, 4), (1, 2000, 96, 32), (1, 1500, 50, 2), (2, 900, 36, 4),
+          (1, 12544, 32, 16), (2, 9001, 24, 8), (1, 3000, 512, 1), (1, 2500, 1040, 2), (1, 6000, 259, 7), (3, 5000, 34, 1), (1, 30000, 3, 1),
+          (2, 1000, 320, 32), (4, 784, 320, 32), (260, 784, 32, 2), (1, 1024, 1024, 1)]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_norm(torch, shape, kind):
+    norm._both(torch, shape, kind, ["none", "relu", "silu"][(shape[1] + shape[2]) % 3])
+
+
+# k of one to four pieces and outputs of one set, several, and sets that are not whole, in few and many rows; rows that end inside a wavefront's
+@pytest.mark.parametrize("rows,k,out", [(64, 128, 64), (65, 100, 30), (130, 256, 200), (1000, 200, 129), (5000, 64, 700), (8192, 300, 100), (8200, 512, 65),
+                                        (17000, 128, 2050), (70000, 40, 70), (20000, 384, 192)])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_linear_short_rows(torch, rows, k, out, kind):
+    act = ["none", "relu", "silu"][(rows + k) % 3]
+    mx._linear(torch, rows, k, out, kind, "f16", act)
+    mx._linear(torch, rows, k, out, kind, "f32", act, quantised=True, out_wide=1)
+
+
+# tiles of 64, 128 and 256 rows and outputs with ends inside them, pieces that fill groups of four and do not, slices of k
+@pytest.mark.parametrize("rows,k,out", [(40, 5000, 520), (70, 1024, 1030), (2000, 640, 2010), (2100, 1500, 2100), (4100, 640, 4200), (4096, 1100, 4096),
+                                        (300, 30000, 40), (2050, 2560, 300)])
+def test_linear_tiles(torch, rows, k, out):
+    mx._linear(torch, rows, k, out, "f16", "bf16", "relu")
+    mx._linear(torch, rows, k, out, "bf16", "f32", "none", quantised=True, bias=False, out_wide=3)
+
+
+def test_linear_few_rows_of_many_values(torch):
+    """x that fits LDS in the workgroups that multiply it, and x that does not."""
+    for rows, k in ((1, 60000), (2, 120000), (9, 25000), (16, 15000), (16, 20000), (3, 300000)):
+        mx._linear(torch, rows, k, 40, "f32", "f32", "none")
+        mx._linear(torch, rows, k, 40, "f16", "f16", "silu", quantised=True)
+
+
+@pytest.mark.parametrize("shape", [(1, 784, 64, 8), (2, 20000, 8, 4)])
+def test_norm_with_something_not_finite(torch, shape):
+    """Held and read twice: what is not finite stays in its group, also where lanes repeat values that count as nothing."""
+    from paper_2001_00138_amd import binding as B
+    n, pixels, c, groups = shape
+    x = torch.randn(n, pixels, c, device="cuda")
+    dy = torch.randn_like(x)
+    want, mean, rstd = B.patdnn_group_norm(x, groups)
+    back, _, _ = B.patdnn_group_norm_backward(dy, x, mean, rstd, groups)
+    per = c // groups
+    for at in ((0, 0, 0), (n - 1, pixels - 1, c - 1), (0, pixels // 2, per)):
+        bad = x.clone()
+        bad[at] = float("inf")
+        hit = torch.zeros_like(x, dtype=torch.bool)
+        hit[at[0], :, at[2] // per * per:(at[2] // per + 1) * per] = True
+        y, _, _ = B.patdnn_group_norm(bad, groups)
+        assert bool(y[hit].isnan().all()) and torch.equal(y[~hit], want[~hit])
+        bad = dy.clone()
+        bad[at] = float("nan")
+        dx, dgamma, dbeta = B.patdnn_group_norm_backward(bad, x, mean, rstd, groups)
+        assert bool(dx[hit].isnan().all()) and torch.equal(dx[~hit], back[~hit])
+        assert dgamma.isnan().sum() == 1 and dbeta.isnan().sum() == 1

@@ -593,44 +593,49 @@ def patdnn_channels_first(x, out=None, *, dtype=None, stream=None):
     return out
 
 
-def _norm_workspace(desc, backward: int, workspace, like, stream):
-    """-> (tensor, its floats)"""
+def _norm_room(desc, backward: int, shape, first, second, workspace, like, stream):
+    """The two small float32 outputs and the workspace of a group norm call, those that are not given allocated (together where the workspace
+    is small: an allocation costs the call 1.5 us, a third of a launch) -> (first, second, workspace's pointer, its floats)."""
     torch = _torch()
-    if workspace is None:
+    if first is None and second is None and workspace is None:
         floats = lib().patdnn_group_norm_workspace_floats(desc, backward)
-        return _new((floats,), torch.float32, like, stream), floats
-    if workspace.dtype != torch.float32:
+        if floats <= 1 << 16:
+            count, strides = (shape[0], (1,)) if len(shape) == 1 else (shape[0] * shape[1], (shape[1], 1))
+            room = _new((floats + 2 * count,), torch.float32, like, stream)
+            return room.as_strided(shape, strides, 0), room.as_strided(shape, strides, count), room.data_ptr() + 8 * count, floats
+        workspace = _new((floats,), torch.float32, like, stream)
+    if first is None:
+        first = _new(shape, torch.float32, like, stream)
+    if second is None:
+        second = _new(shape, torch.float32, like, stream)
+    if workspace is None:
+        workspace = _new((lib().patdnn_group_norm_workspace_floats(desc, backward),), torch.float32, like, stream)
+    elif workspace.dtype != torch.float32:
         raise ValueError("workspace must be a float32 tensor")
-    return workspace, workspace.numel()
+    return first, second, _devptr(workspace), workspace.numel()
 
 
 def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e-5, act="none", mean=None, rstd=None, workspace=None,
                       stream=None):
     """x [n, ..., c] channels last -> (act(group norm) like x, mean, rstd float32 [n, groups]).  gamma, beta: float32 [c] or None.
     x and ``out`` may be slices of the channels of wider tensors."""
-    torch = _torch()
     n, pixels, c, x_image, x_pixel = _channels_last_layout(x, "x")
     if out is None:
         out = _new(tuple(x.shape), x.dtype, x, stream)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("output must have the shape and type of x")
     _, _, _, y_image, y_pixel = _channels_last_layout(out, "output")
-    if mean is None:
-        mean = _new((n, groups), torch.float32, x, stream)
-    if rstd is None:
-        rstd = _new((n, groups), torch.float32, x, stream)
     desc = ctypes.byref(NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), eps, x_image, x_pixel, y_image, y_pixel, 0, 0))
-    workspace, floats = _norm_workspace(desc, 0, workspace, x, stream)
+    mean, rstd, work, floats = _norm_room(desc, 0, (n, max(groups, 0)), mean, rstd, workspace, x, stream)
     _check(lib().patdnn_group_norm(desc, x.data_ptr(), _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"),
                                    out.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
-                                   _devptr(workspace), floats, _stream_ptr(stream)))
+                                   work, floats, _stream_ptr(stream)))
     return out, mean, rstd
 
 
 def patdnn_group_norm_backward(dy, x, mean, rstd, groups: int, gamma=None, beta=None, out=None, *, act="none", dgamma=None, dbeta=None,
                                workspace=None, stream=None):
     """Gradients of patdnn_group_norm: (dx like x, dgamma, dbeta float32 [c]) from dy, x and the forward call's mean and rstd."""
-    torch = _torch()
     n, pixels, c, x_image, x_pixel = _channels_last_layout(x, "x")
     if dy.shape != x.shape or dy.dtype != x.dtype:
         raise ValueError("dy must have the shape and type of x")
@@ -640,16 +645,12 @@ def patdnn_group_norm_backward(dy, x, mean, rstd, groups: int, gamma=None, beta=
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("output must have the shape and type of x")
     _, _, _, y_image, y_pixel = _channels_last_layout(out, "output")
-    if dgamma is None:
-        dgamma = _new((c,), torch.float32, x, stream)
-    if dbeta is None:
-        dbeta = _new((c,), torch.float32, x, stream)
     desc = ctypes.byref(NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), 0.0, x_image, x_pixel, y_image, y_pixel, dy_image, dy_pixel))
-    workspace, floats = _norm_workspace(desc, 1, workspace, x, stream)
+    dgamma, dbeta, work, floats = _norm_room(desc, 1, (c,), dgamma, dbeta, workspace, x, stream)
     _check(lib().patdnn_group_norm_backward(
         desc, dy.data_ptr(), x.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
         _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"), out.data_ptr(), _float_vector(dgamma, c, "dgamma"),
-        _float_vector(dbeta, c, "dbeta"), _devptr(workspace), floats, _stream_ptr(stream)))
+        _float_vector(dbeta, c, "dbeta"), work, floats, _stream_ptr(stream)))
     return out, dgamma, dbeta
 
 

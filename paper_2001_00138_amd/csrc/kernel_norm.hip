@@ -25,7 +25,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 256;          // most channels of a chunk
-constexpr int kMostSlabs = 64;
 constexpr int kAhead = 4;            // pixels a lane has in flight
 
 struct Geometry {
@@ -992,7 +991,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(Geometry G, i
 // ---- launches ----
 
 // Chunks and slabs go by the sizes alone (the workspace's size does too).
-Geometry geometry_of(const NormShape& s)
+Geometry geometry_of(const NormShape& s, bool backward)
 {
     Geometry G{};
     G.s = s;
@@ -1010,9 +1009,10 @@ Geometry geometry_of(const NormShape& s)
         G.per_group = 1;
         G.chunks = (s.c + G.chunk - 1) / G.chunk;
     }
-    // four workgroups a CU if the slabs keep 64 pixels: every workgroup of the second launch adds up all slabs of its image
+    // Four workgroups a CU if the slabs keep 32 pixels, backward 64: every workgroup of the second launch adds up all slabs of its image, backward
+    // per channel (16 x 112x112x64 in groups of two, fp16: 26 us, 37 with twice the slabs; its backward pass in bf16 41 and 103).
     const long long want = 4 * 256 / std::max<long long>(1, (long long)s.n * G.chunks);
-    const int most = (int)std::min<long long>(kMostSlabs, (s.pixels + 63) / 64);
+    const int least = backward ? 64 : 32, most = (int)std::min<long long>(backward ? 64 : 128, (s.pixels + least - 1) / least);
     G.slabs = (int)std::max<long long>(1, std::min<long long>(want, most));
     G.slab = (s.pixels + G.slabs - 1) / G.slabs;
     G.slabs = (s.pixels + G.slab - 1) / G.slab;
@@ -1150,14 +1150,14 @@ int param_blocks_of(const NormShape& s) { return (s.c + kParamChannels - 1) / kP
 
 bool norm_fits(const NormShape& s)
 {
-    const Geometry G = geometry_of(s);
+    const Geometry G = geometry_of(s, false);
     return (long long)s.n * G.chunks <= kMostBlocks && (long long)s.n * G.chunks * G.slabs + param_blocks_of(s) <= kMostBlocks;
 }
 
 size_t norm_workspace_floats(const NormShape& s, bool backward)
 {
     if (s.n == 0) return 0;
-    const Geometry G = geometry_of(s);
+    const Geometry G = geometry_of(s, backward);
     return backward ? (size_t)s.n * G.slabs * 2 * s.c : (size_t)s.n * s.groups * G.slabs * G.per_group * 2;
 }
 
@@ -1194,7 +1194,7 @@ hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, co
         });
         if (e != hipErrorNotReady) return e;
     }
-    Geometry G = geometry_of(s);
+    Geometry G = geometry_of(s, false);
     const int v = run_of(G);
     finish(G, v);
     const dim3 grid((unsigned)(s.n * G.chunks * G.slabs));
@@ -1262,7 +1262,7 @@ hipError_t launch_norm_backward(const NormShape& s, const void* dy, const void* 
         e = hipGetLastError();
     }
     if (e != hipErrorNotReady) return e;
-    Geometry G = geometry_of(s);
+    Geometry G = geometry_of(s, true);
     const int v = run_of(G);
     finish(G, v);
     const unsigned blocks = (unsigned)(s.n * G.chunks * G.slabs);

@@ -133,14 +133,14 @@ hipError_t launch_rows(const LinearShape& s, const void* x, const uint8_t* x_sca
     return hipGetLastError();
 }
 
-// Whether x is quantised where it is multiplied.  16 rows: as long as their codes fit LDS.  Up to 63 (then there is the kernel of short rows): every
-// workgroup quantises its 16 rows, which pays for itself while rows are short and a CU has at most one workgroup (48 x 1024 -> 1000 fp16: 8 us and 11 through tiles;
-// -> 4096 17 and 11; 32 x 4096 -> 1000 14 and 14).
+// Whether x is quantised where it is multiplied, by every workgroup for itself: as long as that takes less than a launch (4 x 4096 -> 4096 fp16: 12 us,
+// 13 with a launch; 16 x 4096 15 and 13, 8 x 25088 30 and 24), and for more than kRows rows, up to 63 (then there is the kernel of short rows), while a CU
+// has at most one workgroup (48 x 1024 -> 1000: 8 us and 11; -> 4096 17 and 11).
 bool in_one_launch(const LinearShape& s)
 {
     if (s.x_type == kMxfp4) return false;
     const long long pieces = mxfp4_pieces(s.in);
-    if (s.rows <= kRows) return s.rows * (pieces * 68 + 16) <= kRowsLds;
+    if (s.rows <= kRows) return (s.rows == 1 || s.rows * pieces <= 256) && s.rows * (pieces * 68 + 16) <= kRowsLds;
     return s.rows < 64 && (pieces <= 4 || (pieces <= 16 && (long long)((s.rows + kRows - 1) / kRows) * ((s.out + 15) / 16) <= 256));
 }
 

@@ -262,14 +262,16 @@ TilePlan tile_plan(const LinearShape& s)
 {
     TilePlan p;
     const long long pieces = mxfp4_pieces(s.in);
-    if (s.rows <= 16 || pieces * 64 * 256 > INT32_MAX) return p;         // offsets in a tile are 32-bit
+    // Four rows are the weights' stream of kernel_linear.hip (16 x 4096 -> 4096 on codes: 17 us there, 11 here).  Offsets in a tile are 32-bit.
+    if (s.rows <= 4 || pieces * 64 * 256 > INT32_MAX) return p;
     auto tiles = [&](int i) { return (long long)((s.out + kShapes[i].bn - 1) / kShapes[i].bn) * ((s.rows + kShapes[i].bm - 1) / kShapes[i].bm); };
+    // The largest tiles that give every CU one (k = 4096, 4096 outputs: 512 rows 12.6, 16 and 32 us with tiles of 64, 128 and 256; 1024 rows 24, 18
+    // and 33; 8192 rows of 8192 values and outputs take the largest).
     p.shape = tiles(0) >= 256 ? 0 : tiles(1) >= 256 ? 1 : 2;
     if (tiles(p.shape) > kMostBlocks / 4) p.shape = -1;
-    else if (p.shape == 2) {
-        const long long groups = (pieces + 3) / 4;
-        p.slices = (int)std::max<long long>(1, std::min<long long>(std::min<long long>(16, groups / 2), 512 / tiles(2)));
-    }
+    // Few tiles are cut along k where a slice keeps 20 stages: adding slices up is a launch of its own (64 x 25088 -> 4096: 43 us in one, 19 in four
+    // and 20 in eight slices; 256 x 4096 -> 4096 10 in one and 17 in two).
+    else if (p.shape == 2) p.slices = (int)std::max<long long>(1, std::min<long long>(std::min<long long>(16, pieces / 20), 512 / tiles(2)));
     return p;
 }
 

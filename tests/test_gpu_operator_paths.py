@@ -78,3 +78,24 @@ def test_norm_with_something_not_finite(torch, shape):
         dx, dgamma, dbeta = B.patdnn_group_norm_backward(bad, x, mean, rstd, groups)
         assert bool(dx[hit].isnan().all()) and torch.equal(dx[~hit], back[~hit])
         assert dgamma.isnan().sum() == 1 and dbeta.isnan().sum() == 1
+
+
+def test_linear_rows_too_long_for_tiles(torch):
+    """Rows whose offsets in a tile would pass 32 bits, against the sum over pieces of k."""
+    from paper_2001_00138_amd import binding as B
+    rows, out, pieces = 17, 5, (1 << 17) + 3
+    g = torch.Generator(device="cuda").manual_seed(4)
+    codes, scales = [], []
+    for count in (rows, out):
+        codes.append(torch.randint(0, 256, (count, pieces * 64), generator=g, device="cuda", dtype=torch.uint8))
+        scales.append(torch.randint(118, 124, (count, pieces * 4), generator=g, device="cuda", dtype=torch.uint8))
+    got = B.patdnn_mxfp4_linear(codes[0], codes[1], scales[1], x_scales=scales[0])
+    want, size = torch.zeros(rows, out, device="cuda", dtype=torch.float64), torch.zeros(rows, out, device="cuda", dtype=torch.float64)
+    step = 8192
+    for p in range(0, pieces, step):
+        part = [B.patdnn_mxfp4_dequantize(c[:, p * 64:(p + step) * 64].contiguous(), s[:, p * 4:(p + step) * 4].contiguous(),
+                                          min(step, pieces - p) * 128).double() for c, s in zip(codes, scales)]
+        want += part[0] @ part[1].t().contiguous()
+        size += part[0].abs() @ part[1].abs().t().contiguous()
+    # a wavefront adds a sixteenth of the pieces, 128 exact products at a time; sixteen such sums are joined
+    assert bool(((got.double() - want).abs() <= (pieces / 16 + 20) * 2.0 ** -24 * size).all())

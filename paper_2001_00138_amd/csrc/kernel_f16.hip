@@ -622,18 +622,18 @@ struct F16Shape {
     hipError_t (*launch[2][2])(const F16Args&, const ConvShape&, long long, size_t, hipStream_t);       // far or not, pairs or not
 };
 // (outputs that need FAR are more than a hundred thousand workgroups of any of the shapes that do not split the channels)
-#define PATDNN_F16(fm, pn, wf, wp, wk, min_blocks, strided) \
+#define F16_SHAPE(fm, pn, wf, wp, wk, min_blocks, strided) \
     {fm, pn, wf, wp, wk, min_blocks, strided, {{&launch_f16_t<fm, pn, wf, wp, wk, false, false>, &launch_f16_t<fm, pn, wf, wp, wk, true, false>}, \
                                                {&launch_f16_t<fm, pn, wf, wp, wk, false, wk == 1>, &launch_f16_t<fm, pn, wf, wp, wk, true, wk == 1>}}}
 static const F16Shape kF16Shapes[] = {
-    PATDNN_F16(2, 4, 2, 2, 1, 256, false),
-    PATDNN_F16(2, 2, 2, 2, 1, 128, true),
-    PATDNN_F16(1, 2, 1, 4, 1, 224, false),
-    PATDNN_F16(1, 2, 1, 1, 4, 400, false),
-    PATDNN_F16(1, 1, 1, 1, 8, 0, false),
-    PATDNN_F16(1, 1, 1, 1, 4, 0, false),
+    F16_SHAPE(2, 4, 2, 2, 1, 256, false),
+    F16_SHAPE(2, 2, 2, 2, 1, 128, true),
+    F16_SHAPE(1, 2, 1, 4, 1, 224, false),
+    F16_SHAPE(1, 2, 1, 1, 4, 400, false),
+    F16_SHAPE(1, 1, 1, 1, 8, 0, false),
+    F16_SHAPE(1, 1, 1, 1, 4, 0, false),
 };
-#undef PATDNN_F16
+#undef F16_SHAPE
 
 // The shape that a launch takes, as an index of kF16Shapes (-1: beyond the kernel's 32-bit numbers).
 struct F16Plan {

@@ -35,7 +35,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_short_kernel(Args A, const
     const uint32_t block = __builtin_amdgcn_readfirstlane((int)fast_div(blockIdx.x, A.by_splits)), split = blockIdx.x - block * (uint32_t)A.splits;
     const int m0 = ((int)block * kWaves + wave) * 16 * kRowTiles;
     if (m0 >= A.s.rows) return;
-    // [tile][piece][row][64 bytes], a row's 16-byte chunks at their place xor row / 4 (banks); then scales [tile][piece][row][4]
+    // [tile][piece][row][64 bytes], a row's 16-byte chunks at their place xor row / 2 (banks); then scales [tile][piece][row][4]
     __shared__ char s_x[kWaves][kRowTiles * P * (1024 + 64)];
     char* const codes = s_x[wave];
     uint8_t* const scales = reinterpret_cast<uint8_t*>(codes + kRowTiles * P * 1024);
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_short_kernel(Args A, const
             for (int t = 0; t < kTogether; ++t)
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    *reinterpret_cast<uint4*>(codes + ((j0 + t) * P + p) * 1024 + r * 64 + (kb ^ (r >> 2)) * 16) = v[t][p];
+                    *reinterpret_cast<uint4*>(codes + ((j0 + t) * P + p) * 1024 + r * 64 + (kb ^ (r >> 1 & 3)) * 16) = v[t][p];
                     scales[((j0 + t) * P + p) * 64 + r * 4 + kb] = (uint8_t)(byte[t].v[p] >> (8 * kb));
                 }
         } else {
@@ -87,14 +87,14 @@ __global__ __launch_bounds__(64 * kWaves) void linear_short_kernel(Args A, const
                         top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
                         top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
                         const uint32_t byte = scale_byte(top);
-                        *reinterpret_cast<uint32_t*>(codes + at * 1024 + (i * 4 + kb) * 64 + ((run >> 2) ^ i) * 16 + (run & 3) * 4) =
+                        *reinterpret_cast<uint32_t*>(codes + at * 1024 + (i * 4 + kb) * 64 + ((run >> 2) ^ (i * 2 + (kb >> 1) & 3)) * 16 + (run & 3) * 4) =
                             byte == kNanScale ? 0u : encode8(v[t][p][i], scale_of(byte));
                         if ((run & 3) == 0) scales[at * 64 + (i * 4 + kb) * 4 + (run >> 2)] = (uint8_t)byte;
                     }
         }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                   // the wavefront's own: no barrier
-    const char* const b_at = codes + r * 64 + (kb ^ (r >> 2)) * 16;
+    const char* const b_at = codes + r * 64 + (kb ^ (r >> 1 & 3)) * 16;
     const uint8_t* const sb_at = scales + r * 4 + kb;
     const int last = A.s.out - 1;
     for (int set = (int)split; set < A.sets; set += A.splits) {

@@ -8,6 +8,7 @@ The package holds:
 * ``binding``    - ctypes marshalling over the C-ABI library ``libpatdnn.so``
   (declared in ``include/patdnn.h``).  Every step of the path runs in the HIP
   library; there is no CPU fallback.
+* ``examples``   - a small network of pruned convolutions, normalisations and 4-bit layers.
 * ``buildlib``   - compiles ``csrc/`` for gfx950 with hipcc.
 * ``profile_summary`` - turns rocprofv3 CSVs into the short summaries kept in
   ``profiles/``.

@@ -8,6 +8,8 @@
 // Few rows: the weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs; its wavefronts
 // take pieces of 128 values of k in turn and add their sums up in LDS, in their order.  A wavefront asks for its first weights, then x is
 // quantised into LDS by all of them (every workgroup does that for itself: there is no launch before), and then weights stream through registers.
+// 1 x 25088 -> 4096: 16 us, 3.4 TB/s of weights: all loads are asked for within the first microseconds, and the launch, the first load's latency
+// and the joining of the sums are not hidden by anything.
 #include <type_traits>
 
 #include "linear.hpp"

@@ -12,10 +12,15 @@
 // lines and channels need no shuffling.  Slabs leave their sums in the workspace; the second launch adds them up
 // in the order of the slabs - the result does not depend on which workgroup came first - and applies them.
 //
-// Statistics are fp32.  Every lane runs Welford's update (mean and sum of squared distances from it), and partial results
-// are joined by Chan's formula: neither subtracts large squares from each other, so values far from zero keep
-// their variance.  With ReLU z is rounded after each of its four operations, forward and backward alike, so
+// Statistics are fp32.  What is held has its mean taken first and then the squared distances from it; where values are seen once, every lane runs
+// Welford's update (mean and sum of squared distances from it), and partial results are joined by Chan's formula: none of them
+// subtracts large squares from each other, so values far from zero keep their variance.  With ReLU z is rounded after each of its four operations, forward and backward alike, so
 // that the two agree about the sign that decides its gradient.
+//
+// Bytes bound it, and for SiLU in two-byte types nearly as much the vector ALU, whose exponential and reciprocal take four cycles each.  64 x 56x56x256:
+// forward fp16 with SiLU 57 us, 3.6 TB/s of the bytes that it cannot do without (held; a workgroup's 16 wavefronts fill a CU's registers, so
+// that loads, arithmetic and stores of a CU overlap little); backward bf16 118 us, 2.6 TB/s, x and dy read twice at 4.3 TB/s; backward
+// fp32 154 us, 4.0 TB/s (held).
 #include "kernels.hpp"
 #include "operators.hpp"
 

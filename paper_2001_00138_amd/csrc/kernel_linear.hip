@@ -8,8 +8,12 @@
 // Few rows: the weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs; its wavefronts
 // take pieces of 128 values of k in turn and add their sums up in LDS, in their order.  A wavefront asks for its first weights, then x is
 // quantised into LDS by all of them (every workgroup does that for itself: there is no launch before), and then weights stream through registers.
-// 1 x 25088 -> 4096: 16 us, 3.4 TB/s of weights: all loads are asked for within the first microseconds, and the launch, the first load's latency
-// and the joining of the sums are not hidden by anything.
+//
+// Two pieces at a time: the sixteen wavefronts of a workgroup, and with few registers two workgroups a CU, have enough loads on their way, and asking
+// for more before x is there only delays it and asks for the last pieces again (fp16, us with 2, 4 and 8 pieces: 1 x 25088 -> 4096 13.5, 14.1 and 16.2;
+// 4 x 4096 -> 4096 5.3, 7.0 and 10.5; 1 x 8192 -> 8192 12.5, 10.7 and 19.0; 1 x 25088 -> 16384 48, 51 and 63; with eight wavefronts 14.7, 6.0, 11.9
+// and 52 at 2 pieces).  1 x 25088 -> 4096: 13.4 us, 4.1 TB/s of weights; the launch, the first load's latency and the joining of the sums are not
+// hidden by anything.
 #include <type_traits>
 
 #include "linear.hpp"
@@ -21,7 +25,7 @@ namespace {
 struct Codes {};                                         // x is MXFP4 already
 
 constexpr int kRows = 16;                                // most rows of x here: the matrix instruction's
-constexpr int kAhead = 8;                                // pieces of weights that a wavefront has on their way
+constexpr int kAhead = 2;                                // pieces of weights that a wavefront asks for together
 constexpr int kRowsLds = 128 * 1024;                     // most bytes of x in LDS
 
 struct Args {
@@ -135,15 +139,24 @@ hipError_t launch_rows(const LinearShape& s, const void* x, const uint8_t* x_sca
     return hipGetLastError();
 }
 
-// Whether x is quantised where it is multiplied, by every workgroup for itself: as long as that takes less than a launch (4 x 4096 -> 4096 fp16: 12 us,
-// 13 with a launch; 16 x 4096 15 and 13, 8 x 25088 30 and 24), and for more than kRows rows, up to 63 (then there is the kernel of short rows), while a CU
-// has at most one workgroup (48 x 1024 -> 1000: 8 us and 11; -> 4096 17 and 11).
+int workgroups_of(const LinearShape& s) { return (s.rows + kRows - 1) / kRows * ((s.out + 15) / 16); }
+
+// Whether codes are multiplied here and not in tiles: up to four rows, and up to 63 (many rows of few values are the kernel of short rows) while a CU has
+// at most one workgroup, which reads the weights once, and k is no longer than 64 pieces (codes -> fp16, us here and in tiles: 16 x 4096 -> 4096 6.2 and
+// 9.1, 48 x 4096 -> 1000 6.0 and 9.0, 16 x 8192 -> 1000 9.1 and 10.0; above: 20 x 1024 -> 4096 5.7 and 4.1, 5 x 2048 -> 6000 7.1 and 5.6,
+// 16 x 12288 -> 4096 12.9 and 12.1, 8 x 25088 -> 1000 16.5 and 13.4).
+bool by_rows(const LinearShape& s) { return s.rows <= 4 || (s.rows < 64 && workgroups_of(s) <= 256 && mxfp4_pieces(s.in) <= 64); }
+
+// Whether x is quantised where it is multiplied, by every workgroup for itself.  That is less than a launch up to some 400 pieces (fp16, us in one
+// launch and in two: 12 x 4096 -> 1000 7.3 and 7.7, 16 x 4096 8.5 and 8.0; 2 x 25088 -> 4096 15.2 and 16.3, 4 x 25088 19.2 and 17.2); from five rows on
+// also while a CU has at most one workgroup or all of them together have few weights to read (63 x 512 -> 4096 5.7 and 5.8, 32 x 1024 -> 4096 6.2 and
+// 6.5; 48 x 1024 -> 4096 8.0 and 6.6, 5 x 1024 -> 16384 7.1 and 6.8).  One row is: 1 x 25088 -> 4096 13.3 and 15.3.
 bool in_one_launch(const LinearShape& s)
 {
-    if (s.x_type == kMxfp4) return false;
-    const long long pieces = mxfp4_pieces(s.in);
-    if (s.rows <= kRows) return (s.rows == 1 || s.rows * pieces <= 256) && s.rows * (pieces * 68 + 16) <= kRowsLds;
-    return s.rows < 64 && (pieces <= 4 || (pieces <= 16 && (long long)((s.rows + kRows - 1) / kRows) * ((s.out + 15) / 16) <= 256));
+    if (s.x_type == kMxfp4 || s.rows >= 64) return false;
+    const long long pieces = mxfp4_pieces(s.in), rows = std::min(s.rows, kRows);
+    if (rows * (pieces * 68 + 16) > kRowsLds || (s.rows > 1 && rows * pieces > 400)) return false;
+    return s.rows <= 4 || workgroups_of(s) <= 256 || workgroups_of(s) * pieces <= 4096;
 }
 
 }  // namespace
@@ -167,7 +180,7 @@ Room room_of(const LinearShape& s)
     Room r{};
     if (short_fits(s)) return r;
     r.quantised_here = s.x_type != kMxfp4 && !in_one_launch(s);
-    r.plan = tile_plan(s);
+    if (!by_rows(s)) r.plan = tile_plan(s);
     // (more than kRows rows: room for the codes whichever way the call takes, so that a change of that choice is no caller's concern)
     const size_t blocks = r.quantised_here || (s.x_type != kMxfp4 && s.rows > kRows) ? (size_t)s.rows * (size_t)mxfp4_pieces(s.in) * 4 : 0;
     r.scales_at = blocks * 16;

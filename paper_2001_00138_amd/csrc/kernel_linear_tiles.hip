@@ -282,8 +282,7 @@ TilePlan tile_plan(const LinearShape& s)
 {
     TilePlan p;
     const long long pieces = mxfp4_pieces(s.in);
-    // Four rows are the weights' stream of kernel_linear.hip (16 x 4096 -> 4096 on codes: 17 us there, 11 here).  Offsets in a tile are 32-bit.
-    if (s.rows <= 4 || pieces * 64 * 256 > INT32_MAX) return p;
+    if (pieces * 64 * 256 > INT32_MAX) return p;         // offsets in a tile are 32-bit
     auto tiles = [&](int i) { return (long long)((s.out + kShapes[i].bn - 1) / kShapes[i].bn) * ((s.rows + kShapes[i].bm - 1) / kShapes[i].bm); };
     // The largest tiles that give every CU one (k = 4096, 4096 outputs: 512 rows 12.6, 16 and 32 us with tiles of 64, 128 and 256; 1024 rows 24, 18
     // and 33; 8192 rows of 8192 values and outputs take the largest).

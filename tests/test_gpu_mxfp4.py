@@ -155,6 +155,14 @@ def test_linear_larger(torch, rows, k, out):
     _linear(torch, rows, k, out, "bf16", "bf16", "relu", quantised=True)
 
 
+# few rows on either side of each choice: in one launch or two, by rows or in tiles, with one and more tiles of rows
+@pytest.mark.parametrize("rows,k,out", [(4, 12900, 33), (4, 12700, 33), (5, 300, 4200), (20, 300, 4112), (63, 500, 4400), (20, 1500, 2100), (20, 2100, 2100), (13, 5000, 900),
+                                        (12, 4100, 900), (48, 4100, 700), (37, 4200, 1400), (63, 8192, 70), (63, 8193, 70), (17, 8300, 70)])
+def test_linear_few_rows(torch, rows, k, out):
+    _linear(torch, rows, k, out, "f16", "f32", "silu")
+    _linear(torch, rows, k, out, "f32", "f16", "none", quantised=True)
+
+
 @pytest.mark.parametrize("rows", [2, 40, 300])
 def test_linear_is_exact_where_sums_are(torch, rows):
     """Small whole numbers: every sum is exact, whatever its order, so outputs are equal."""

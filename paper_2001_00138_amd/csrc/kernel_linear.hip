@@ -163,7 +163,7 @@ bool in_one_launch(const LinearShape& s)
 
 bool linear_fits(const LinearShape& s)
 {
-    return mxfp4_pieces(s.in) * 128 <= INT32_MAX - 128 && (long long)((s.rows + 15) / 16) * ((s.out + 15) / 16) <= kMostBlocks / 4 &&
+    return mxfp4_pieces(s.in) * 128 <= INT32_MAX - 128 && (s.rows + 15ll) / 16 * ((s.out + 15ll) / 16) <= kMostBlocks / 4 &&
            mxfp4_fits(Mxfp4Shape{s.rows, s.in, kF32, s.in});
 }
 

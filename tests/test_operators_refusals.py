@@ -107,6 +107,23 @@ def test_linear():
     assert f(_linear(rows=0), None, None, None, None, None, None, None, 0, None) == B.PATDNN_OK
 
 
+@pytest.mark.parametrize("rows", [1, 4, 20, 2 ** 20])
+@pytest.mark.parametrize("out", [2 ** 31 - 1, 2 ** 31 - 15, 2 ** 27])
+def test_linear_with_too_many_outputs(rows, out):
+    """Outputs whose tiles do not fit a grid, the last ones of a C int among them: no workspace is asked for."""
+    many = _linear(rows=rows, out_features=out, out_row=out)
+    assert L().patdnn_mxfp4_linear_workspace_bytes(many) == 0
+    _refused(B.PATDNN_EUNSUPPORTED, "large", L().patdnn_mxfp4_linear, many, P, None, Q, Q + 4096, None, R, S, 1 << 20, None)
+
+
+@pytest.mark.parametrize("out", [5, 40])
+@pytest.mark.parametrize("rows", [2 ** 31 - 1, 2 ** 31 - 15])
+def test_linear_with_too_many_rows(rows, out):
+    many = _linear(rows=rows, out_features=out, out_row=out)
+    assert L().patdnn_mxfp4_linear_workspace_bytes(many) == 0
+    _refused(B.PATDNN_EUNSUPPORTED, "large", L().patdnn_mxfp4_linear, many, P, None, Q, Q + 4096, None, R, S, 1 << 20, None)
+
+
 def test_the_binding():
     import torch
     x = torch.zeros(2, 4, 4, 8)

@@ -5,7 +5,7 @@
 // rows lie in memory.  The weights are the instruction's first operand, so that a lane's four results are
 // neighbours along n.  Sums are fp32.
 //
-// Few rows: the weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs; its wavefronts
+// Few rows, or few outputs: the weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs; its wavefronts
 // take pieces of 128 values of k in turn and add their sums up in LDS, in their order.  A wavefront asks for its first weights, then x is
 // quantised into LDS by all of them (every workgroup does that for itself: there is no launch before), and then weights stream through registers.
 //
@@ -139,21 +139,21 @@ hipError_t launch_rows(const LinearShape& s, const void* x, const uint8_t* x_sca
     return hipGetLastError();
 }
 
-int workgroups_of(const LinearShape& s) { return (s.rows + kRows - 1) / kRows * ((s.out + 15) / 16); }
+long long workgroups_of(const LinearShape& s) { return (s.rows + kRows - 1ll) / kRows * ((s.out + 15ll) / 16); }
 
-// Whether codes are multiplied here and not in tiles: up to four rows, and up to 63 (many rows of few values are the kernel of short rows) while a CU has
-// at most one workgroup, which reads the weights once, and k is no longer than 64 pieces (codes -> fp16, us here and in tiles: 16 x 4096 -> 4096 6.2 and
-// 9.1, 48 x 4096 -> 1000 6.0 and 9.0, 16 x 8192 -> 1000 9.1 and 10.0; above: 20 x 1024 -> 4096 5.7 and 4.1, 5 x 2048 -> 6000 7.1 and 5.6,
-// 16 x 12288 -> 4096 12.9 and 12.1, 8 x 25088 -> 1000 16.5 and 13.4).
-bool by_rows(const LinearShape& s) { return s.rows <= 4 || (s.rows < 64 && workgroups_of(s) <= 256 && mxfp4_pieces(s.in) <= 64); }
+// Whether codes are multiplied here and not in tiles: up to four rows, and while a CU has at most one workgroup and k is no longer than 64 pieces (codes
+// -> fp16, us here and in tiles: 16 x 4096 -> 4096 6.2 and 9.1, 48 x 4096 -> 1000 6.0 and 9.0, 256 x 4100 -> 256 4.5 and 9.5, 3000 x 8192 -> 16 9.1 and
+// 10.1; above: 77 x 2048 -> 1000 9.2 and 6.2, 5 x 2048 -> 6000 7.1 and 5.6, 16 x 12288 -> 4096 12.9 and 12.1, 8 x 25088 -> 1000 16.5 and 13.4).
+bool by_rows(const LinearShape& s) { return s.rows <= 4 || (workgroups_of(s) <= 256 && mxfp4_pieces(s.in) <= 64); }
 
 // Whether x is quantised where it is multiplied, by every workgroup for itself.  That is less than a launch up to some 400 pieces (fp16, us in one
-// launch and in two: 12 x 4096 -> 1000 7.3 and 7.7, 16 x 4096 8.5 and 8.0; 2 x 25088 -> 4096 15.2 and 16.3, 4 x 25088 19.2 and 17.2); from five rows on
-// also while a CU has at most one workgroup or all of them together have few weights to read (63 x 512 -> 4096 5.7 and 5.8, 32 x 1024 -> 4096 6.2 and
-// 6.5; 48 x 1024 -> 4096 8.0 and 6.6, 5 x 1024 -> 16384 7.1 and 6.8).  One row is: 1 x 25088 -> 4096 13.3 and 15.3.
+// launch and in two: 12 x 4096 -> 1000 7.3 and 7.7, 16 x 4096 8.5 and 8.0; 128 x 2048 -> 500 6.4 and 8.0; 2 x 25088 -> 4096 15.2 and 16.3, 4 x 25088 19.2
+// and 17.2); from five rows on also while a CU has at most one workgroup or all of them together have few weights to read (63 x 512 -> 4096 5.7 and 5.8,
+// 77 x 1024 -> 1000 6.1 and 7.3, 32 x 1024 -> 4096 6.2 and 6.5; 48 x 1024 -> 4096 8.0 and 6.6, 5 x 1024 -> 16384 7.1 and 6.8).  One row always is:
+// 1 x 25088 -> 4096 13.3 and 15.3.
 bool in_one_launch(const LinearShape& s)
 {
-    if (s.x_type == kMxfp4 || s.rows >= 64) return false;
+    if (s.x_type == kMxfp4) return false;
     const long long pieces = mxfp4_pieces(s.in), rows = std::min(s.rows, kRows);
     if (rows * (pieces * 68 + 16) > kRowsLds || (s.rows > 1 && rows * pieces > 400)) return false;
     return s.rows <= 4 || workgroups_of(s) <= 256 || workgroups_of(s) * pieces <= 4096;
@@ -163,7 +163,7 @@ bool in_one_launch(const LinearShape& s)
 
 bool linear_fits(const LinearShape& s)
 {
-    return mxfp4_pieces(s.in) * 128 <= INT32_MAX - 128 && (s.rows + 15ll) / 16 * ((s.out + 15ll) / 16) <= kMostBlocks / 4 &&
+    return mxfp4_pieces(s.in) * 128 <= INT32_MAX - 128 && workgroups_of(s) <= kMostBlocks / 4 &&
            mxfp4_fits(Mxfp4Shape{s.rows, s.in, kF32, s.in});
 }
 

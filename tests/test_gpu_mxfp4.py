@@ -163,6 +163,16 @@ def test_linear_few_rows(torch, rows, k, out):
     _linear(torch, rows, k, out, "f32", "f16", "none", quantised=True)
 
 
+# more outputs or rows than a workgroup a CU takes: tiles, of every size and with their ends inside
+@pytest.mark.parametrize("rows", [5, 17, 64, 77, 130, 300, 1025])
+@pytest.mark.parametrize("k,out", [(1, 4400), (515, 4099), (1300, 4112), (2100, 4353), (2600, 1030), (8200, 270)])
+def test_linear_many_outputs(torch, rows, k, out):
+    kinds = KINDS[(rows + k) % 3], KINDS[(rows + out) % 3]
+    _linear(torch, rows, k, out, *kinds, ["none", "relu", "silu"][(rows + k + out) % 3], quantised=True)
+    if (rows + out) % 2:
+        _linear(torch, rows, k, out, *kinds, "relu", out_wide=3, x_wide=5)
+
+
 @pytest.mark.parametrize("rows", [2, 40, 300])
 def test_linear_is_exact_where_sums_are(torch, rows):
     """Small whole numbers: every sum is exact, whatever its order, so outputs are equal."""

@@ -292,8 +292,7 @@ struct Held {
 };
 
 // Most runs that a lane holds, so that nothing spills: of 16 bytes, of eight, of fewer.
-template <class T, int V>
-constexpr int held_runs() { return V * sizeof(T) >= 16 ? 16 : V * sizeof(T) == 8 ? 24 : 32; }
+constexpr int held_runs(int run_bytes) { return run_bytes >= 16 ? 16 : run_bytes == 8 ? 24 : 32; }
 
 __device__ __forceinline__ uint32_t held_block(uint32_t total)
 {
@@ -658,18 +657,21 @@ __global__ __launch_bounds__(kThreads) void norm_params_kernel(int channels, int
     add_params(channels, images, (int)blockIdx.x * kParamChannels, parts, s_a, s_b, dgamma, dbeta);
 }
 
-// Runs of dy that the kernel below keeps in LDS.
-template <int R>
-constexpr int held_in_lds() { return R > 8 ? 9 : 0; }
+// Runs of dy that the kernel below keeps in LDS, with room for r.
+constexpr int held_in_lds(int r) { return r > 8 ? 9 : 0; }
+// Most runs of x and dy that a lane holds.  Two-byte values: eight runs take as long as reading twice where thirteen do not fit the registers any
+// more.  And where a lane's channels are of several groups, with statistics for each.
+constexpr int held_back_runs(int type_bytes) { return type_bytes == 4 ? 13 : 8; }
+constexpr int held_back_mixed_runs(int type_bytes) { return type_bytes == 4 ? 8 : 4; }
 
-// The backward pass of what norm_held_kernel does.  x and dy are both held: R runs of either, of dy the first held_in_lds<R>() in LDS.
+// The backward pass of what norm_held_kernel does.  x and dy are both held: R runs of either, of dy the first held_in_lds(R) in LDS.
 // sums_a, sums_b: dz and dz xh over an image's pixels, per channel, images 2 * channels floats apart.
 template <class T, int V, int R, bool ONE>
 __global__ __launch_bounds__(1024) void norm_back_held_kernel(Held G, const T* __restrict__ dy, const T* __restrict__ x, const float* __restrict__ mean_in,
                                                               const float* __restrict__ rstd_in, const float* __restrict__ gamma,
                                                               const float* __restrict__ beta, T* __restrict__ dx, float* __restrict__ sums_a, float* __restrict__ sums_b)
 {
-    constexpr int kInLds = held_in_lds<R>(), M = ONE ? 1 : V;
+    constexpr int kInLds = held_in_lds(R), M = ONE ? 1 : V;
     using Run = Kept<T, V>;
     extern __shared__ float shared[];
     const uint32_t block = held_block(gridDim.x);
@@ -1140,7 +1142,7 @@ hipError_t launch_held_back(const Held& H, int threads, const void* dy, const vo
                             const float* beta, void* dx, float* sums_a, float* sums_b, hipStream_t stream)
 {
     static std::atomic<uint64_t> allowed{0};
-    const size_t lds = held_back_lds(H, V, threads, held_in_lds<R>(), sizeof(Kept<T, V>));
+    const size_t lds = held_back_lds(H, V, threads, held_in_lds(R), sizeof(Kept<T, V>));
     if (lds > 64 * 1024)
         if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(norm_back_held_kernel<T, V, R, ONE>), allowed); e != hipSuccess) return e;
     hipLaunchKernelGGL((norm_back_held_kernel<T, V, R, ONE>), dim3((unsigned)(H.s.n * H.chunks)), dim3((unsigned)threads), lds, stream, H,
@@ -1151,7 +1153,57 @@ hipError_t launch_held_back(const Held& H, int threads, const void* dy, const vo
 
 int param_blocks_of(const NormShape& s) { return (s.c + kParamChannels - 1) / kParamChannels; }
 
+// What a call launches: the held kernel for lanes of `v` channels with room for `room` runs, or (v = 0) two launches.
+struct Plan {
+    Held H{};
+    int v = 0, threads = 0, runs = 0, room = 0;
+    bool one = false;                                    // the kernels' ONE
+};
+
+Plan plan_of(const NormShape& s)
+{
+    Plan p;
+    for (int v = run_of(s); v > 0; v /= 2) {
+        const int most = held_runs(v * (int)element_bytes(s.type));
+        if (!held_of(s, v, most, false, p.H, p.threads, p.runs)) continue;
+        p.v = v;
+        p.one = p.H.cpg % v == 0;
+        p.room = p.runs <= 2 ? 2 : p.runs <= most / 4 ? most / 4 : p.runs <= most / 2 ? most / 2 : p.runs <= most * 3 / 4 + 1 ? most * 3 / 4 + 1 : most;
+        break;
+    }
+    return p;
+}
+
+// Held where lanes have whole runs of 16 bytes, and sums fold or pixels are few: the other way to add columns up costs more than reading
+// twice (8 x 56x56x64 in groups of two, fp32: 23 us and 15).
+Plan back_plan_of(const NormShape& s)
+{
+    Plan p;
+    const int bytes = (int)element_bytes(s.type), v = 16 / bytes, most = held_back_runs(bytes);
+    if (run_of(s) != v) return p;
+    p.one = s.c / s.groups % v == 0;
+    // more constants a lane: fewer runs
+    if (!held_of(s, v, p.one ? most : held_back_mixed_runs(bytes), true, p.H, p.threads, p.runs)) return p;
+    p.room = p.runs <= 2 ? 2 : p.runs <= 4 ? 4 : p.runs <= 8 ? 8 : most;
+    if (!p.one && p.room > held_back_mixed_runs(bytes)) return p;          // no such kernel
+    // (64 x 56x56x256 bf16, 32 bytes a pixel: 135 us held, 118 in two launches)
+    if ((!p.H.folded && (s.pixels > 1024 || p.runs > 8)) || (p.H.chunk * bytes < 64 && (long long)s.n * p.H.chunks >= 256) ||
+        held_back_lds(p.H, v, p.threads, held_in_lds(p.room), 16) > 160 * 1024)
+        return p;
+    p.v = v;
+    return p;
+}
+
 }  // namespace
+
+// For tests: lanes' channels (0: two launches), runs, room for runs, whether lanes keep to one group, threads, rows of lanes, channels of a chunk, bytes of LDS.
+void norm_plan_numbers(const NormShape& s, bool backward, int32_t (&out)[8])
+{
+    const Plan p = backward ? back_plan_of(s) : plan_of(s);
+    const size_t lds = !p.v ? 0 : backward ? held_back_lds(p.H, p.v, p.threads, held_in_lds(p.room), 16) : held_lds(p.H, p.v, p.threads);
+    const int32_t numbers[8] = {p.v, p.runs, p.room, p.one, p.threads, p.H.ty, p.H.chunk, (int32_t)lds};
+    std::copy(numbers, numbers + 8, out);
+}
 
 bool norm_fits(const NormShape& s)
 {
@@ -1169,35 +1221,32 @@ size_t norm_workspace_floats(const NormShape& s, bool backward)
 hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd,
                        float* workspace, hipStream_t stream)
 {
-    for (int v = run_of(s); v > 0; v /= 2) {
-        hipError_t e = hipErrorNotReady;
+    if (const Plan p = plan_of(s); p.v) {
+        hipError_t e = hipErrorInvalidValue;
         with_type(s.type, [&](auto t) {
             using T = decltype(t);
-            with_run(v, [&](auto run) {
+            with_run(p.v, [&](auto run) {
                 constexpr int V = decltype(run)::value;
                 if constexpr (V * sizeof(T) <= 16) {
-                    constexpr int kMost = held_runs<T, V>();
-                    Held H;
-                    int threads, runs;
-                    if (!held_of(s, V, kMost, false, H, threads, runs)) return;
-                    auto with_runs = [&](auto r) {
+                    constexpr int kMost = held_runs(V * sizeof(T));
+                    auto with_room = [&](auto r) {
                         constexpr int R = decltype(r)::value;
                         if constexpr (V > 1)
-                            if (H.cpg % V) {
-                                e = launch_held<T, V, R, false>(H, threads, x, gamma, beta, y, mean, rstd, stream);
+                            if (!p.one) {
+                                e = launch_held<T, V, R, false>(p.H, p.threads, x, gamma, beta, y, mean, rstd, stream);
                                 return;
                             }
-                        e = launch_held<T, V, R, true>(H, threads, x, gamma, beta, y, mean, rstd, stream);
+                        e = launch_held<T, V, R, true>(p.H, p.threads, x, gamma, beta, y, mean, rstd, stream);
                     };
-                    if (runs <= 2) with_runs(Const<2>{});
-                    else if (runs <= kMost / 4) with_runs(Const<kMost / 4>{});
-                    else if (runs <= kMost / 2) with_runs(Const<kMost / 2>{});
-                    else if (runs <= kMost * 3 / 4 + 1) with_runs(Const<kMost * 3 / 4 + 1>{});
-                    else with_runs(Const<kMost>{});
+                    if (p.room == 2) with_room(Const<2>{});
+                    else if (p.room == kMost / 4) with_room(Const<kMost / 4>{});
+                    else if (p.room == kMost / 2) with_room(Const<kMost / 2>{});
+                    else if (p.room == kMost * 3 / 4 + 1) with_room(Const<kMost * 3 / 4 + 1>{});
+                    else with_room(Const<kMost>{});
                 }
             });
         });
-        if (e != hipErrorNotReady) return e;
+        return e;
     }
     Geometry G = geometry_of(s, false);
     const int v = run_of(G);
@@ -1222,51 +1271,35 @@ hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, co
 hipError_t launch_norm_backward(const NormShape& s, const void* dy, const void* x, const float* mean, const float* rstd, const float* gamma,
                                 const float* beta, void* dx, float* dgamma, float* dbeta, float* workspace, hipStream_t stream)
 {
-    hipError_t e;
+    hipError_t e = hipErrorInvalidValue;
     if (s.n == 0) {                                      // sums over nothing
         if (dgamma && (e = launch_fill_zero(dgamma, (size_t)s.c, stream)) != hipSuccess) return e;
         if (dbeta && (e = launch_fill_zero(dbeta, (size_t)s.c, stream)) != hipSuccess) return e;
         return hipSuccess;
     }
-    // Held where lanes have whole runs of 16 bytes, and sums fold or pixels are few: the other way to add columns up costs more than reading
-    // twice (8 x 56x56x64 in groups of two, fp32: 23 us and 15).
-    e = hipErrorNotReady;
-    // one image: its sums are dbeta and dgamma
-    float* const sums_a = s.n == 1 && dbeta ? dbeta : workspace;
-    float* const sums_b = s.n == 1 && dgamma ? dgamma : workspace + s.c;
-    with_type(s.type, [&](auto t) {
-        using T = decltype(t);
-        constexpr int V = 16 / (int)sizeof(T);
-        // two-byte values: eight runs take as long as reading twice where thirteen do not fit the registers any more
-        constexpr int kMost = sizeof(T) == 4 ? 13 : 8;
-        if (run_of(s) != V) return;
-        Held H;
-        int threads, runs;
-        const int fewer = s.c / s.groups % V == 0 ? kMost : sizeof(T) == 4 ? 8 : 4;      // more constants a lane: fewer runs
-        // (64 x 56x56x256 bf16, 32 bytes a pixel: 135 us held, 118 in two launches)
-        if (!held_of(s, V, fewer, true, H, threads, runs) || (!H.folded && (s.pixels > 1024 || runs > 8)) ||
-            (H.chunk * sizeof(T) < 64 && (long long)s.n * H.chunks >= 256) ||
-            held_back_lds(H, V, threads, runs > 8 ? held_in_lds<kMost>() : 0, sizeof(Kept<T, V>)) > 160 * 1024)
-            return;
-        auto with_runs = [&](auto r) {
-            constexpr int R = decltype(r)::value;
-            if constexpr (R <= (sizeof(T) == 4 ? 8 : 4))
-                if (H.cpg % V) {
-                    e = launch_held_back<T, V, R, false>(H, threads, dy, x, mean, rstd, gamma, beta, dx, sums_a, sums_b, stream);
-                    return;
-                }
-            e = launch_held_back<T, V, R, true>(H, threads, dy, x, mean, rstd, gamma, beta, dx, sums_a, sums_b, stream);
-        };
-        if (runs <= 2) with_runs(Const<2>{});
-        else if (runs <= 4) with_runs(Const<4>{});
-        else if (runs <= 8) with_runs(Const<8>{});
-        else with_runs(Const<kMost>{});
-    });
-    if (e == hipSuccess && s.n > 1 && (dgamma || dbeta)) {
-        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)param_blocks_of(s)), dim3(kThreads), 0, stream, s.c, s.n, workspace, dgamma, dbeta);
-        e = hipGetLastError();
+    if (const Plan p = back_plan_of(s); p.v) {
+        // one image: its sums are dbeta and dgamma
+        float* const sums_a = s.n == 1 && dbeta ? dbeta : workspace;
+        float* const sums_b = s.n == 1 && dgamma ? dgamma : workspace + s.c;
+        with_type(s.type, [&](auto t) {
+            using T = decltype(t);
+            constexpr int V = 16 / (int)sizeof(T), kMost = held_back_runs(sizeof(T)), kMixed = held_back_mixed_runs(sizeof(T));
+            auto with_room = [&](auto r) {
+                constexpr int R = decltype(r)::value;
+                if (p.one) e = launch_held_back<T, V, R, true>(p.H, p.threads, dy, x, mean, rstd, gamma, beta, dx, sums_a, sums_b, stream);
+                else if constexpr (R <= kMixed) e = launch_held_back<T, V, R, false>(p.H, p.threads, dy, x, mean, rstd, gamma, beta, dx, sums_a, sums_b, stream);
+            };
+            if (p.room == 2) with_room(Const<2>{});
+            else if (p.room == 4) with_room(Const<4>{});
+            else if (p.room == 8) with_room(Const<8>{});
+            else with_room(Const<kMost>{});
+        });
+        if (e == hipSuccess && s.n > 1 && (dgamma || dbeta)) {
+            hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)param_blocks_of(s)), dim3(kThreads), 0, stream, s.c, s.n, workspace, dgamma, dbeta);
+            e = hipGetLastError();
+        }
+        return e;
     }
-    if (e != hipErrorNotReady) return e;
     Geometry G = geometry_of(s, true);
     const int v = run_of(G);
     finish(G, v);

@@ -30,6 +30,7 @@ struct NormShape {
 };
 size_t norm_workspace_floats(const NormShape& s, bool backward);
 bool norm_fits(const NormShape& s);
+void norm_plan_numbers(const NormShape& s, bool backward, int32_t (&out)[8]);
 hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd,
                        float* workspace, hipStream_t stream);
 // y_* of the shape are dx's strides here.

@@ -219,6 +219,17 @@ patdnn_status_t patdnn_group_norm_backward(const patdnn_norm_desc_t* desc, const
                 "launching the group norm's backward pass");
 }
 
+// For tests: how a call would be launched (norm_plan_numbers).
+patdnn_status_t patdnn_internal_norm_plan(const patdnn_norm_desc_t* desc, int32_t backward, int32_t out[8])
+{
+    NormShape s{};
+    int32_t numbers[8] = {};
+    const patdnn_status_t st = norm_shape(desc, backward != 0, s);
+    if (st == PATDNN_OK) norm_plan_numbers(s, backward != 0, numbers);
+    for (int i = 0; i < 8; ++i) out[i] = numbers[i];
+    return st;
+}
+
 patdnn_status_t patdnn_mxfp4_quantize(const void* x, int32_t type, int32_t rows, int32_t cols, int64_t row, uint8_t* codes, uint8_t* scales,
                                       void* stream)
 {

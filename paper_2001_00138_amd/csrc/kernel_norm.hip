@@ -1090,6 +1090,8 @@ bool held_of(const NormShape& s, int v, int most, bool backward, Held& H, int& t
     // workgroups share a CU.  (64 x 14x14x1024 fp16: 34 us with one run a lane, 16 with four.)
     const long long need = (long long)H.tx * s.pixels / ((long long)s.n * H.chunks < 512 ? 1 : std::min(most, backward ? 8 : 4));
     threads = (int)std::max<long long>((H.tx + 63) / 64 * 64, std::min<long long>(1024, (need + 63) / 64 * 64));
+    // `need` is rounded down, and so are the rows of lanes: more lanes where that leaves runs without room (1024 have room: fits())
+    while ((s.pixels + threads / H.tx - 1) / (threads / H.tx) > most) threads += 64;
     H.ty = threads / H.tx;
     runs = H.runs = (s.pixels + H.ty - 1) / H.ty;
     H.full = s.pixels - (H.runs - 1) * H.ty;

@@ -50,3 +50,19 @@ def test_one_statistic_for_channels_of_one_group(shapes, kind, backward):
         several = not p["one"] and (not backward or p["room"] <= 4 * (BYTES[kind] // 2))
         assert several or (c // groups) % p["v"] == 0, (n, pixels, c, groups, p)
     assert held > 1000
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_a_lane_has_room_for_its_runs(shapes, kind, backward):
+    held = 0
+    for n, pixels, c, groups in shapes:
+        p = _plan(n, pixels, c, groups, kind, backward)
+        if not p["v"]:
+            continue
+        held += 1
+        case = (n, pixels, c, groups, p)
+        assert p["rows"] * p["runs"] >= pixels > p["rows"] * (p["runs"] - 1) and p["runs"] <= p["room"], case
+        assert p["chunk"] % p["v"] == 0 and p["chunk"] % (c // groups) == 0 and p["rows"] * (p["chunk"] // p["v"]) <= p["threads"], case
+        assert p["threads"] % 64 == 0 and p["threads"] <= 1024 and p["lds"] <= 160 * 1024, case
+    assert held > 1000

@@ -595,14 +595,15 @@ def patdnn_channels_first(x, out=None, *, dtype=None, stream=None):
 
 def _norm_room(desc, backward: int, shape, first, second, workspace, like, stream):
     """The two small float32 outputs and the workspace of a group norm call, those that are not given allocated (together where the workspace
-    is small: an allocation costs the call 1.5 us, a third of a launch) -> (first, second, workspace's pointer, its floats)."""
+    is small: an allocation costs the call 1.5 us, a third of a launch) -> (first, second, workspace's pointer, its floats, its owner).  The owner
+    must be held until the call has returned: on the stream of the launches, freed memory is the next allocation's, also another thread's."""
     torch = _torch()
     if first is None and second is None and workspace is None:
         floats = lib().patdnn_group_norm_workspace_floats(desc, backward)
         if floats <= 1 << 16:
             count, strides = (shape[0], (1,)) if len(shape) == 1 else (shape[0] * shape[1], (shape[1], 1))
             room = _new((floats + 2 * count,), torch.float32, like, stream)
-            return room.as_strided(shape, strides, 0), room.as_strided(shape, strides, count), room.data_ptr() + 8 * count, floats
+            return room.as_strided(shape, strides, 0), room.as_strided(shape, strides, count), room.data_ptr() + 8 * count, floats, room
         workspace = _new((floats,), torch.float32, like, stream)
     if first is None:
         first = _new(shape, torch.float32, like, stream)
@@ -612,7 +613,7 @@ def _norm_room(desc, backward: int, shape, first, second, workspace, like, strea
         workspace = _new((lib().patdnn_group_norm_workspace_floats(desc, backward),), torch.float32, like, stream)
     elif workspace.dtype != torch.float32:
         raise ValueError("workspace must be a float32 tensor")
-    return first, second, _devptr(workspace), workspace.numel()
+    return first, second, _devptr(workspace), workspace.numel(), workspace
 
 
 def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e-5, act="none", mean=None, rstd=None, workspace=None,
@@ -626,10 +627,11 @@ def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e
         raise ValueError("output must have the shape and type of x")
     _, _, _, y_image, y_pixel = _channels_last_layout(out, "output")
     desc = ctypes.byref(NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), eps, x_image, x_pixel, y_image, y_pixel, 0, 0))
-    mean, rstd, work, floats = _norm_room(desc, 0, (n, max(groups, 0)), mean, rstd, workspace, x, stream)
+    mean, rstd, work, floats, owner = _norm_room(desc, 0, (n, max(groups, 0)), mean, rstd, workspace, x, stream)
     _check(lib().patdnn_group_norm(desc, x.data_ptr(), _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"),
                                    out.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
                                    work, floats, _stream_ptr(stream)))
+    del owner
     return out, mean, rstd
 
 
@@ -646,11 +648,12 @@ def patdnn_group_norm_backward(dy, x, mean, rstd, groups: int, gamma=None, beta=
         raise ValueError("output must have the shape and type of x")
     _, _, _, y_image, y_pixel = _channels_last_layout(out, "output")
     desc = ctypes.byref(NormDesc(n, pixels, c, groups, _type(x.dtype), _act(act), 0.0, x_image, x_pixel, y_image, y_pixel, dy_image, dy_pixel))
-    dgamma, dbeta, work, floats = _norm_room(desc, 1, (c,), dgamma, dbeta, workspace, x, stream)
+    dgamma, dbeta, work, floats, owner = _norm_room(desc, 1, (c,), dgamma, dbeta, workspace, x, stream)
     _check(lib().patdnn_group_norm_backward(
         desc, dy.data_ptr(), x.data_ptr(), _float_vector(mean, n * groups, "mean"), _float_vector(rstd, n * groups, "rstd"),
         _float_vector(gamma, c, "gamma"), _float_vector(beta, c, "beta"), out.data_ptr(), _float_vector(dgamma, c, "dgamma"),
         _float_vector(dbeta, c, "dbeta"), work, floats, _stream_ptr(stream)))
+    del owner
     return out, dgamma, dbeta
 
 

@@ -493,6 +493,8 @@ patdnn_status_t patdnn_channels_first(const void* input, int32_t in_type, int64_
  *   dgamma, dbeta [channels] or NULL; written, not added to (zeros for n == 0)
  *   workspace     patdnn_group_norm_workspace_floats floats, contents undefined before and after
  * Results repeat bit for bit.  groups divides channels; n == 0 is a no-op but for dgamma and dbeta.
+ * PATDNN_EUNSUPPORTED beyond 2^31 - 1025 pixels and beyond 2^24 workgroups of a launch (one for every 16 channels and every 256 channels of
+ * an image).
  */
 typedef struct {
     int32_t n, pixels, channels, groups;

@@ -1022,7 +1022,7 @@ Geometry geometry_of(const NormShape& s, bool backward)
     const int least = backward ? 64 : 32, most = (int)std::min<long long>(backward ? 64 : 128, (s.pixels + least - 1) / least);
     G.slabs = (int)std::max<long long>(1, std::min<long long>(want, most));
     G.slab = (s.pixels + G.slabs - 1) / G.slabs;
-    G.slabs = (s.pixels + G.slab - 1) / G.slab;
+    G.slabs = (int)ceil_div(s.pixels, G.slab);
     G.inv_m = (float)(1.0 / ((double)s.pixels * G.cpg));
     return G;
 }
@@ -1083,7 +1083,7 @@ bool held_of(const NormShape& s, int v, int most, bool backward, Held& H, int& t
     if (H.chunk * element_bytes(s.type) < 32 && s.pixels > (backward ? 4096 : 8192)) return false;
     // 64 adjacent bytes a pixel, as long as every CU has a workgroup
     while (H.chunk * element_bytes(s.type) < 64 && H.chunk * 2 <= s.c && fits(H.chunk * 2) && (long long)s.n * (s.c / (H.chunk * 2)) >= 256) H.chunk *= 2;
-    H.chunks = (s.c + H.chunk - 1) / H.chunk;
+    H.chunks = (int)ceil_div(s.c, H.chunk);
     if ((long long)s.n * H.chunks > kMostBlocks / 4) return false;
     H.tx = H.chunk / v;
     // Every lane has one run where there are few workgroups; where there are many, four (eight where x and dy are held), and several
@@ -1161,7 +1161,6 @@ struct Plan {
     int v = 0, threads = 0, runs = 0, room = 0;
     bool one = false;                                    // the kernels' ONE
 };
-
 Plan plan_of(const NormShape& s)
 {
     Plan p;
@@ -1209,6 +1208,8 @@ void norm_plan_numbers(const NormShape& s, bool backward, int32_t (&out)[8])
 
 bool norm_fits(const NormShape& s)
 {
+    // 32-bit sums here and in the kernels go past the pixels and channels by as much as a workgroup has lanes
+    if (s.pixels > kMostNormLength || s.c > kMostNormLength) return false;
     const Geometry G = geometry_of(s, false);
     return (long long)s.n * G.chunks <= kMostBlocks && (long long)s.n * G.chunks * G.slabs + param_blocks_of(s) <= kMostBlocks;
 }

@@ -13,6 +13,8 @@ namespace patdnn {
 // Most workgroups of 256 threads that one launch may have (a grid has fewer than 2^32 threads).
 constexpr long long kMostBlocks = (1ll << 24) - 1;
 
+inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
 // ---- order of channels (kernel_reorder.hip) ----
 // out[b][j][i] = in[b][i][j]: `rows` x `cols` of each of `batch` matrices; strides in elements, columns adjacent.
 struct TransposeShape {
@@ -28,8 +30,10 @@ struct NormShape {
     float eps;
     long long x_image, x_pixel, y_image, y_pixel, dy_image, dy_pixel;      // strides in elements
 };
-size_t norm_workspace_floats(const NormShape& s, bool backward);
+constexpr int kMostNormLength = INT32_MAX - 1024;        // pixels, and channels
 bool norm_fits(const NormShape& s);
+// (the rest only for what fits)
+size_t norm_workspace_floats(const NormShape& s, bool backward);
 void norm_plan_numbers(const NormShape& s, bool backward, int32_t (&out)[8]);
 hipError_t launch_norm(const NormShape& s, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd,
                        float* workspace, hipStream_t stream);

@@ -523,6 +523,7 @@ patdnn_status_t patdnn_group_norm_backward(const patdnn_norm_desc_t* desc, const
  * a value becomes the nearest code to value / 2^(b - 127), ties to the even code, magnitudes above 6 become 6.
  * A block that holds something not finite has b = 255 and zero codes; its values read back as NaN.
  *   x / out: `type`, `row` elements between rows (out: >= cols), values of a row adjacent.
+ * PATDNN_EUNSUPPORTED beyond 2^24 workgroups of 2048 values (each of whole rows, or of part of one).
  * rows == 0 is a no-op.
  */
 patdnn_status_t patdnn_mxfp4_quantize(const void* x, int32_t type, int32_t rows, int32_t cols, int64_t row, uint8_t* codes,

@@ -32,7 +32,7 @@ Spread spread_of(const Mxfp4Shape& s)
 long long blocks_of(const Mxfp4Shape& s)
 {
     const Spread p = spread_of(s);
-    return (long long)p.blocks_across * ((s.rows + p.down - 1) / p.down);
+    return p.blocks_across * ceil_div(s.rows, p.down);
 }
 
 // This thread's row and run; false if it has none.

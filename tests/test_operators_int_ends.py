@@ -45,3 +45,13 @@ def test_norm_as_long_as_it_goes(pixels, c, groups, kind):
         out = (ctypes.c_int32 * 8)()
         assert L().patdnn_internal_norm_plan(d, backward, out) == B.PATDNN_OK
         assert out[0] == 0                                 # nothing of that size is held in registers
+
+
+@pytest.mark.parametrize("rows", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 31 - 15, 2 ** 31 - 16, 2 ** 31 - 100, 2 ** 28])
+@pytest.mark.parametrize("cols", [1, 128, 129, 2048, 2049])
+def test_quantise_too_many_rows(rows, cols):
+    """No rows of memory but the first: a row for all to quantise, of strides of zero."""
+    assert L().patdnn_mxfp4_quantize(P, 0, rows, cols, 0, 1 << 50, 1 << 51, None) == B.PATDNN_EUNSUPPORTED
+    assert "large" in L().patdnn_last_error().decode()
+    assert L().patdnn_mxfp4_dequantize(1 << 50, 1 << 51, rows, cols, P, 1, cols, None) == B.PATDNN_EUNSUPPORTED
+    assert "large" in L().patdnn_last_error().decode()

@@ -540,7 +540,8 @@ patdnn_status_t patdnn_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sca
  *   bias         fp32 [out_features] or NULL
  *   workspace    patdnn_mxfp4_linear_workspace_bytes bytes, 16-byte aligned (may be NULL if that is 0), contents
  *                undefined before and after; calls that share one must not overlap in time
- * Results repeat bit for bit.  rows == 0 is a no-op.
+ * Results repeat bit for bit.  rows == 0 is a no-op.  PATDNN_EUNSUPPORTED beyond 2^26 outputs, 2^31 - 257 rows, and where a launch would have more
+ * than some 2^22 workgroups (of 256 x 256 outputs; up to 512 input features are bounded by rows and outputs only).
  */
 typedef struct {
     int32_t rows, in_features, out_features;

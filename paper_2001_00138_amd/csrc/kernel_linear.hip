@@ -161,12 +161,6 @@ bool in_one_launch(const LinearShape& s)
 
 }  // namespace
 
-bool linear_fits(const LinearShape& s)
-{
-    return mxfp4_pieces(s.in) * 128 <= INT32_MAX - 128 && workgroups_of(s) <= kMostBlocks / 4 &&
-           mxfp4_fits(Mxfp4Shape{s.rows, s.in, kF32, s.in});
-}
-
 namespace {
 
 // The workspace: codes and scales of x where it is quantised in a launch of its own, then the slices' sums.
@@ -190,6 +184,17 @@ Room room_of(const LinearShape& s)
 }
 
 }  // namespace
+
+// Outputs that one row can have (a workgroup for 16 of them), whatever the rows; rows that 32-bit sums of a tile's end do not pass (so the kernel of short
+// rows has fewer than 2^24 workgroups, of 128 rows and more); and the grids of what is launched.
+bool linear_fits(const LinearShape& s)
+{
+    if (mxfp4_pieces(s.in) * 128 > INT32_MAX - 128 || ceil_div(s.out, 16) > kMostBlocks / 4 || s.rows > INT32_MAX - 256) return false;
+    if (short_fits(s)) return true;
+    const Room room = room_of(s);
+    return (!room.quantised_here || mxfp4_fits(Mxfp4Shape{s.rows, s.in, s.x_type, s.x_row})) &&
+           (room.plan.shape >= 0 || workgroups_of(s) <= kMostBlocks / 4);
+}
 
 size_t linear_workspace_bytes(const LinearShape& s) { return room_of(s).bytes; }
 

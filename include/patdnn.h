@@ -448,8 +448,8 @@ patdnn_status_t patdnn_stack_run_static(patdnn_stack_t s, const float* input, fl
  * What stands between and behind the 3x3 convolutions of a network: the order of channels, group
  * normalisation, and linear layers (pointwise convolutions are linear layers whose rows are pixels) on
  * weights of four bits.  No handles: all memory is the caller's, every call is asynchronous on
- * `stream`, allocates nothing and never synchronises.  Outputs must not overlap inputs, counted from a tensor's first
- * to its last element.  All pointers DEVICE and aligned to their elements unless said otherwise.
+ * `stream`, allocates nothing and never synchronises.  Outputs and the workspace must not overlap inputs or one another, counted
+ * from a tensor's first to its last element.  All pointers DEVICE and aligned to their elements unless said otherwise.
  * ---------------------------------------------------------------------------------------------
  */
 

@@ -1,5 +1,6 @@
 // C entry points of the operators around the convolutions (include/patdnn.h): checks of the arguments, and the launches.
 #include <cmath>
+#include <initializer_list>
 #include <new>
 #include <string>
 
@@ -57,6 +58,17 @@ bool overlap(const Span& a, const Span& b)
     const char* p = static_cast<const char*>(a.p);
     const char* q = static_cast<const char*>(b.p);
     return p && q && p < q + b.bytes && q < p + a.bytes;
+}
+// Whether an output shares memory with an input or with another output (NULL: not there).
+bool outputs_overlap(std::initializer_list<Span> inputs, std::initializer_list<Span> outputs)
+{
+    for (const Span& a : outputs) {
+        for (const Span& b : inputs)
+            if (overlap(a, b)) return true;
+        for (const Span& b : outputs)
+            if (&a != &b && overlap(a, b)) return true;
+    }
+    return false;
 }
 
 patdnn_status_t reorder(bool last, const void* in, int32_t in_type, int32_t n, int32_t channels, int32_t pixels, void* out, int32_t out_type,
@@ -190,6 +202,9 @@ patdnn_status_t patdnn_group_norm(const patdnn_norm_desc_t* desc, const void* x,
     if (const patdnn_status_t st = check_workspace(workspace, workspace_floats, needs, "patdnn_group_norm_workspace_floats")) return st;
     const Span work{workspace, (long long)needs * 4};
     if (overlap(work, in) || overlap(work, out)) return fail(PATDNN_EINVAL, "workspace overlaps input or output");
+    const long long channels = 4ll * s.c, statistics = 4ll * s.n * s.groups;
+    if (outputs_overlap({in, {gamma, channels}, {beta, channels}}, {out, work, {mean, statistics}, {rstd, statistics}}))
+        return fail(PATDNN_EINVAL, "an output or the workspace overlaps another tensor");
     return done(launch_norm(s, x, gamma, beta, y, mean, rstd, workspace, static_cast<hipStream_t>(stream)), "launching the group norm");
 }
 
@@ -214,6 +229,10 @@ patdnn_status_t patdnn_group_norm_backward(const patdnn_norm_desc_t* desc, const
         if (const patdnn_status_t st = check_workspace(workspace, workspace_floats, needs, "patdnn_group_norm_workspace_floats")) return st;
         const Span work{workspace, (long long)needs * 4};
         if (overlap(work, in) || overlap(work, grad) || overlap(work, out)) return fail(PATDNN_EINVAL, "workspace overlaps input or output");
+        const long long channels = 4ll * s.c, statistics = 4ll * s.n * s.groups;
+        if (outputs_overlap({in, grad, {mean, statistics}, {rstd, statistics}, {gamma, channels}, {beta, channels}},
+                            {out, work, {dgamma, channels}, {dbeta, channels}}))
+            return fail(PATDNN_EINVAL, "an output or the workspace overlaps another tensor");
     }
     return done(launch_norm_backward(s, dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta, workspace, static_cast<hipStream_t>(stream)),
                 "launching the group norm's backward pass");

@@ -31,15 +31,19 @@ struct Args {
 constexpr int kBand = 8;                                 // rows of tiles that are taken side by side
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// Moves 16 (4) bytes a lane from memory to LDS: lane l's to lds + 16 l (4 l), the start from m0, which nothing else here uses.  Not waited for:
-// s_waitcnt vmcnt counts it.
+// Moves 16 (4) bytes a lane from memory to LDS: lane l's to lds + 16 l (4 l), the start from m0, which the compiler keeps for itself and finds as it
+// was (the load reads it as it is issued).  Not waited for: s_waitcnt vmcnt counts it.
 __device__ __forceinline__ void fetch16(intx4 buffer, uint32_t lds, uint32_t lane_offset, uint32_t offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(lane_offset), "s"(buffer), "s"(offset) : "memory");
+    uint32_t kept;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(lds), "v"(lane_offset), "s"(buffer), "s"(offset) : "memory");
 }
 __device__ __forceinline__ void fetch4(intx4 buffer, uint32_t lds, uint32_t lane_offset, uint32_t offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(lane_offset), "s"(buffer), "s"(offset) : "memory");
+    uint32_t kept;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(lds), "v"(lane_offset), "s"(buffer), "s"(offset) : "memory");
 }
 template <int OUTSTANDING>
 __device__ __forceinline__ void wait_fetches()

@@ -21,6 +21,8 @@
 // forward fp16 with SiLU 57 us, 3.6 TB/s of the bytes that it cannot do without (held; a workgroup's 16 wavefronts fill a CU's registers, so
 // that loads, arithmetic and stores of a CU overlap little); backward bf16 118 us, 2.6 TB/s, x and dy read twice at 4.3 TB/s; backward
 // fp32 154 us, 4.0 TB/s (held).
+#include <type_traits>
+
 #include "kernels.hpp"
 #include "operators.hpp"
 
@@ -121,6 +123,7 @@ __device__ __forceinline__ void walk(const T* p, long long step, int count, F&& 
         Pack<T, V> v[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) v[u] = load_pack<T, V>(p + u * step);
+        __builtin_amdgcn_sched_barrier(0);               // all of them before the first is used
         p += kAhead * step;
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -211,17 +214,17 @@ __device__ __forceinline__ float affine(float d, float rstd, float gamma, float 
     return d * rstd * gamma + beta;
 }
 
-// Without ReLU nothing jumps where z is 0, and z = x a + b takes one operation instead of four: a = rstd gamma and b = beta - mean a go into
-// gamma's and beta's places.
-__device__ __forceinline__ void straight(float mean, float rstd, float& gamma, float& beta)
+// Without ReLU nothing jumps where z is 0: (x - mean) scale + beta with scale = rstd gamma, as the backward pass has it.  (x scale + (beta - mean scale)
+// would be an operation less, but rounds at the size of mean scale: values far from zero would lose what x - mean keeps.)
+// (binary16: x * 1 - mean takes x as it is stored, with a 1 that the compiler does not know; in fp32 x would be widened first.  64 x 56x56x256 with SiLU:
+// 50.4 us with five tensors in turn, 51.9 widened.)
+template <class T, int ACT>
+__device__ __forceinline__ float apply_one(float x, float mean, float rstd, float gamma, float beta, float scale)
 {
-    gamma *= rstd;
-    beta = fmaf(-mean, gamma, beta);
-}
-template <int ACT>
-__device__ __forceinline__ float apply_one(float x, float mean, float rstd, float gamma, float beta)
-{
-    return activate<ACT>(ACT == kActRelu ? affine(centred(x, mean), rstd, gamma, beta) : fmaf(x, gamma, beta));
+    float one = 1.0f;
+    if (std::is_same_v<T, _Float16>) asm("" : "+s"(one));
+    const float d = std::is_same_v<T, _Float16> ? fmaf(x, one, -mean) : centred(x, mean);
+    return activate<ACT>(ACT == kActRelu ? affine(d, rstd, gamma, beta) : fmaf(d, scale, beta));
 }
 
 template <class T, int V, int ACT>
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Geometry G, const 
     const int ty = (int)fast_div(threadIdx.x, G.by_tx), tx = (int)threadIdx.x - ty * G.tx;
     const int c = tx * V, first = w.p0 + ty;
     if (ty >= G.ty || c >= w.width || first >= w.p1) return;
-    float mean[V], rstd[V], ga[V], be[V];
+    float mean[V], rstd[V], ga[V], be[V], scale[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int g = G.per_group == 1 ? (int)fast_div((uint32_t)(c + i), G.by_cpg) : 0;
@@ -265,13 +268,13 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Geometry G, const 
         rstd[i] = s_rstd[g];
         ga[i] = gamma ? gamma[w.c0 + c + i] : 1.0f;
         be[i] = beta ? beta[w.c0 + c + i] : 0.0f;
-        if (ACT != kActRelu) straight(mean[i], rstd[i], ga[i], be[i]);
+        scale[i] = rstd[i] * ga[i];
     }
     T* to = y + w.n * G.s.y_image + first * G.s.y_pixel + w.c0 + c;
     walk<T, V>(x + w.n * G.s.x_image + first * G.s.x_pixel + w.c0 + c, G.ty * G.s.x_pixel, (w.p1 - first + G.ty - 1) / G.ty, [&](const float (&v)[V]) {
         Pack<T, V> r;
 #pragma unroll
-        for (int i = 0; i < V; ++i) r.v[i] = from_float<T>(apply_one<ACT>(v[i], mean[i], rstd[i], ga[i], be[i]));
+        for (int i = 0; i < V; ++i) r.v[i] = from_float<T>(apply_one<T, ACT>(v[i], mean[i], rstd[i], ga[i], be[i], scale[i]));
         store_pack<T, V>(to, r);
         to += G.ty * G.s.y_pixel;
     });
@@ -503,15 +506,15 @@ __global__ __launch_bounds__(1024) void norm_held_kernel(Held G, const T* __rest
     const long long y_step = G.ty * G.s.y_pixel;
     auto apply = [&](auto act) {
         constexpr int ACT = decltype(act)::value;
-        if (ACT != kActRelu)
+        float scale[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) straight(mean[ONE ? 0 : i], rstd[ONE ? 0 : i], ga[i], be[i]);
+        for (int i = 0; i < V; ++i) scale[i] = rstd[ONE ? 0 : i] * ga[i];
 #pragma unroll
         for (int k = 0; k < R; ++k)
             if (k < count) {
                 Pack<T, V> r;
 #pragma unroll
-                for (int i = 0; i < V; ++i) r.v[i] = from_float<T>(apply_one<ACT>(kept[k].at(i), mean[ONE ? 0 : i], rstd[ONE ? 0 : i], ga[i], be[i]));
+                for (int i = 0; i < V; ++i) r.v[i] = from_float<T>(apply_one<T, ACT>(kept[k].at(i), mean[ONE ? 0 : i], rstd[ONE ? 0 : i], ga[i], be[i], scale[i]));
                 store_pack<T, V>(to, r);
                 to += y_step;
                 __builtin_amdgcn_sched_barrier(0);       // one run's values at a time

@@ -449,7 +449,7 @@ patdnn_status_t patdnn_stack_run_static(patdnn_stack_t s, const float* input, fl
  * normalisation, and linear layers (pointwise convolutions are linear layers whose rows are pixels) on
  * weights of four bits.  No handles: all memory is the caller's, every call is asynchronous on
  * `stream`, allocates nothing and never synchronises.  Outputs and the workspace must not overlap inputs or one another, counted
- * from a tensor's first to its last element.  All pointers DEVICE and aligned to their elements unless said otherwise.
+ * from a tensor's first to its last element; an output may be another slice of the wide tensor that an input is a slice of.  All pointers DEVICE and aligned to their elements unless said otherwise.
  * ---------------------------------------------------------------------------------------------
  */
 

@@ -40,24 +40,32 @@ patdnn_status_t done(hipError_t e, const char* what)
 bool real_type(int32_t t) { return t == kF32 || t == kF16 || t == kBF16; }
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
-// A strided tensor [n][pixels][channels], or [1][rows][values].
+// A strided tensor [n][pixels][channels], or [1][rows][values]: its bytes from the first element to the last, in runs of `width` that all start a
+// multiple of `pitch` behind the first (0: not in such a rhythm).
 struct Span {
     const void* p;
-    long long bytes;
+    long long bytes, pitch = 0, width = 0;
 };
-// Elements from the first to the last; false if they are more than addresses can count.
+// False if the elements from the first to the last are more than addresses can count.
 bool span_of(long long n, long long image, long long pixels, long long pixel, long long channels, int type, const void* p, Span& s)
 {
     const __int128 elements = (__int128)(n - 1) * image + (__int128)(pixels - 1) * pixel + channels;
     if (elements > ((__int128)1 << 56)) return false;
-    s = Span{p, (long long)elements * (long long)element_bytes(type)};
+    const long long size = (long long)element_bytes(type);
+    s = Span{p, (long long)elements * size};
+    const long long pitch = pixels > 1 ? pixel : n > 1 ? image : 0;
+    if (pitch && (n == 1 || image % pitch == 0)) s.pitch = pitch * size, s.width = channels * size;
     return true;
 }
 bool overlap(const Span& a, const Span& b)
 {
     const char* p = static_cast<const char*>(a.p);
     const char* q = static_cast<const char*>(b.p);
-    return p && q && p < q + b.bytes && q < p + a.bytes;
+    if (!(p && q && p < q + b.bytes && q < p + a.bytes)) return false;
+    if (!a.pitch || a.pitch != b.pitch) return true;
+    // slices of one wider tensor: b's runs start `d` behind a's
+    const long long ahead = (q - p) % a.pitch, d = ahead < 0 ? ahead + a.pitch : ahead;
+    return d < a.width || d + b.width > a.pitch;
 }
 // Whether an output shares memory with an input or with another output (NULL: not there).
 bool outputs_overlap(std::initializer_list<Span> inputs, std::initializer_list<Span> outputs)

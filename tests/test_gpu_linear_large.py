@@ -54,3 +54,22 @@ def test_many_outputs(torch):
     check()
     for a, b in _parts(out, 4096):
         assert torch.equal(y[:, a:b], B.patdnn_mxfp4_linear(x, w[a:b], w_scales[a:b], x_scales=scales, dtype=torch.bfloat16)), (a, b)
+
+
+# every number of pieces with every number of rows a wavefront: work is sets of 64 rows times sets of 64 outputs, up to 1024, and from 8192 on with 32 sets of outputs
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("rows,out", [(8200, 65), (8200, 1025), (16400, 2050)])
+@pytest.mark.parametrize("k", [100, 200, 300, 500])
+def test_short_rows_are_exact_where_sums_are(torch, rows, k, out, kind):
+    """Small whole numbers: every sum is exact, so results are equal to the product."""
+    g = torch.Generator(device="cuda").manual_seed(10)
+    x, w = (torch.randint(-3, 4, (count, k), generator=g, device="cuda").float() for count in (rows, out))
+    x[:, ::32], w[:, ::32] = 4, 4                              # units of 1 in every block
+    want = (x.double() @ w.double().t().contiguous()).float()
+    codes = B.patdnn_mxfp4_quantize(w)
+    x = x.to(getattr(torch, kind))
+    y, check = guarded(torch, (rows, out), torch.float32)
+    assert torch.equal(B.patdnn_mxfp4_linear(x, *codes, out=y), want)
+    check()
+    xc, xs = B.patdnn_mxfp4_quantize(x)
+    assert torch.equal(B.patdnn_mxfp4_linear(xc, *codes, x_scales=xs, act="relu"), want.relu())

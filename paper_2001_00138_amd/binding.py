@@ -619,7 +619,8 @@ def _norm_room(desc, backward: int, shape, first, second, workspace, like, strea
 def patdnn_group_norm(x, groups: int, gamma=None, beta=None, out=None, *, eps=1e-5, act="none", mean=None, rstd=None, workspace=None,
                       stream=None):
     """x [n, ..., c] channels last -> (act(group norm) like x, mean, rstd float32 [n, groups]).  gamma, beta: float32 [c] or None.
-    x and ``out`` may be slices of the channels of wider tensors."""
+    x and ``out`` may be slices of the channels of wider tensors, also of one.  Where the call allocates all of mean, rstd and its workspace, mean and rstd
+    are views of one allocation, which lives as long as they do (up to 256 KB more than they hold)."""
     n, pixels, c, x_image, x_pixel = _channels_last_layout(x, "x")
     if out is None:
         out = _new(tuple(x.shape), x.dtype, x, stream)

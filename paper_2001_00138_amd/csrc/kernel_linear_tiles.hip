@@ -11,8 +11,8 @@
 // rows so that a lane's results for four tiles are sixteen neighbouring outputs: whole runs are stored without going
 // through LDS.
 //
-// 8192 x 8192 values, 8192 outputs, bf16: 290 us, 3.8 PFLOP/s.  The matrix cores are busy 48 % of the cycles, at 1.75 GHz of 2.4: the card's power
-// bounds it, the more the less the wavefronts wait.
+// 8192 x 8192 values, 8192 outputs, bf16: 290 us, 3.8 PFLOP/s.  The matrix cores are busy 48 % of the cycles, at 1.75 GHz of 2.4 (which points to the
+// card's power, but was not shown: with fewer LDS conflicts the clock fell from 1.85 GHz, and all wavefronts together still waited as long).
 #include "linear.hpp"
 
 namespace patdnn {

@@ -18,7 +18,7 @@
 // that the two agree about the sign that decides its gradient.
 //
 // Bytes bound it, and for SiLU in two-byte types nearly as much the vector ALU, whose exponential and reciprocal take four cycles each.  64 x 56x56x256:
-// forward fp16 with SiLU 57 us, 3.6 TB/s of the bytes that it cannot do without (held; a workgroup's 16 wavefronts fill a CU's registers, so
+// forward fp16 with SiLU 58 us, 3.5 TB/s of the bytes that it cannot do without (held; a workgroup's 16 wavefronts fill a CU's registers, so
 // that loads, arithmetic and stores of a CU overlap little); backward bf16 118 us, 2.6 TB/s, x and dy read twice at 4.3 TB/s; backward
 // fp32 154 us, 4.0 TB/s (held).
 #include <type_traits>
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(Geometry G, const 
         for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.0f;
         walk<T, V>(x + w.n * G.s.x_image + first * G.s.x_pixel + w.c0 + c, G.ty * G.s.x_pixel, count, [&](const float (&v)[V]) {
             n += 1.0f;
-            const float share = __builtin_amdgcn_rcpf(n);
+            const float share = __builtin_amdgcn_rcpf(n);        // (off by 2^-23 of a step that moves the mean by less than a deviation / n)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float d = v[i] - mean[i];

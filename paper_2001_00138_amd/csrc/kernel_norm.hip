@@ -43,7 +43,7 @@ struct Geometry {
     int join;                        // lanes that join the sums of one group (a power of two up to 64)
     int runs, full, last_runs, last_full;        // pixels that the first `full` rows of lanes have, the others one less; of the last slab
     int width, parts;                // channels of a chunk that is whole, and how often a workgroup has a lane for each
-    float inv_m;                     // 1 / (pixels * cpg)
+    float m;                         // pixels * cpg.  (Divided by: a product with the rounded 1 / m would make the mean of equal values another one.)
     FastDiv by_slabs, by_chunks, by_tx, by_cpg, by_width;
 };
 
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Geometry G, const 
                 si = from[2 * i + 1];
             }, mean, m2);
             if (lane == 0) {
-                const float rstd = 1.0f / sqrtf(m2 * G.inv_m + G.s.eps);
+                const float rstd = 1.0f / sqrtf(m2 / G.m + G.s.eps);
                 s_mean[g] = mean;
                 s_rstd[g] = rstd;
                 if (w.part == 0) {
@@ -289,7 +289,7 @@ struct Held {
     int span, entries;                                   // channels of a lane that are joined before others see them; what a row of lanes adds to a group
     int folded, lanes;                                   // a group's lanes in a row are a power of two (`lanes`), and the rows too: sums fold by exchange
     int runs, full;                                      // runs that the first `full` rows of lanes have, the others one less
-    float inv_m;
+    float m;
     int parts;                                           // into which the backward kernel cuts the rows of lanes where it adds columns up
     FastDiv by_chunks, by_tx, by_cpg, by_entries, by_chunk;
 };
@@ -411,11 +411,11 @@ __global__ __launch_bounds__(1024) void norm_held_kernel(Held G, const T* __rest
         const int wave = (int)threadIdx.x >> 6, waves = (int)blockDim.x >> 6;
         const bool folded = ONE && G.folded;
         if (folded) {
-            sum[0] = fold(G, sum[0], c, groups, wave, waves, s_part) * G.inv_m;
+            sum[0] = fold(G, sum[0], c, groups, wave, waves, s_part) / G.m;
         } else {
-            const float share = count ? 1.0f / (float)(ONE ? count * V : count) : 0.0f;
+            const float many = (float)max(1, ONE ? count * V : count);
 #pragma unroll
-            for (int i = 0; i < M; ++i) sum[i] *= share;
+            for (int i = 0; i < M; ++i) sum[i] /= many;
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(1024) void norm_held_kernel(Held G, const T* __rest
         if (folded) {
             m2[0] = fold(G, m2[0], c, groups, wave, waves, s_part + waves * groups);
             mean[0] = sum[0];
-            rstd[0] = 1.0f / sqrtf(m2[0] * G.inv_m + G.s.eps);
+            rstd[0] = 1.0f / sqrtf(m2[0] / G.m + G.s.eps);
             const int g = (int)fast_div((uint32_t)c, G.by_cpg);
             if (ty == 0 && count && c == g * G.cpg) {
                 const long long at = (long long)n * G.s.groups + g0 + g;
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(1024) void norm_held_kernel(Held G, const T* __rest
                     si = s_m2[at];
                 }, mean_g, m2_g);
                 if (lane == 0) {
-                    const float rstd_g = 1.0f / sqrtf(m2_g * G.inv_m + G.s.eps);
+                    const float rstd_g = 1.0f / sqrtf(m2_g / G.m + G.s.eps);
                     const long long at = (long long)n * G.s.groups + g0 + g;
                     g_mean[g] = mean_g;
                     g_rstd[g] = rstd_g;
@@ -800,8 +800,8 @@ __global__ __launch_bounds__(1024) void norm_back_held_kernel(Held G, const T* _
             for (int k = 0; k < waves; ++k) v += s_channel[(k * 2 + half) * G.chunk + at];
             if (at < width) (half ? to_b : to_a)[at] = v;
         }
-        shift[0] = rstd[0] * (ag * G.inv_m);
-        slope[0] = rstd[0] * rstd[0] * (bg * G.inv_m);
+        shift[0] = rstd[0] * (ag / G.m);
+        slope[0] = rstd[0] * rstd[0] * (bg / G.m);
     } else {
         const int pitch = G.tx * V, all = G.ty * pitch;
         float* const s_a = s;                            // [row of lanes][channel]
@@ -852,8 +852,8 @@ __global__ __launch_bounds__(1024) void norm_back_held_kernel(Held G, const T* _
             ag = lanes_sum(ag, G.join);
             bg = lanes_sum(bg, G.join);
             if (lane == 0) {
-                g_a[g] = ag * G.inv_m;
-                g_b[g] = bg * G.inv_m;
+                g_a[g] = ag / G.m;
+                g_b[g] = bg / G.m;
             }
         }
         __syncthreads();
@@ -935,8 +935,8 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(Geometry G, i
             a = lanes_sum(a, G.join);
             b = lanes_sum(b, G.join);
             if (lane == 0) {
-                g_a[g] = a * G.inv_m;
-                g_b[g] = b * G.inv_m;
+                g_a[g] = a / G.m;
+                g_b[g] = b / G.m;
             }
         }
     } else {
@@ -964,8 +964,8 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(Geometry G, i
                 a += s_a[k];
                 b += s_b[k];
             }
-            g_a[0] = a * G.inv_m;
-            g_b[0] = b * G.inv_m;
+            g_a[0] = a / G.m;
+            g_b[0] = b / G.m;
         }
     }
     __syncthreads();
@@ -1026,7 +1026,7 @@ Geometry geometry_of(const NormShape& s, bool backward)
     G.slabs = (int)std::max<long long>(1, std::min<long long>(want, most));
     G.slab = (s.pixels + G.slabs - 1) / G.slabs;
     G.slabs = (int)ceil_div(s.pixels, G.slab);
-    G.inv_m = (float)(1.0 / ((double)s.pixels * G.cpg));
+    G.m = (float)((double)s.pixels * G.cpg);
     return G;
 }
 
@@ -1098,7 +1098,7 @@ bool held_of(const NormShape& s, int v, int most, bool backward, Held& H, int& t
     H.ty = threads / H.tx;
     runs = H.runs = (s.pixels + H.ty - 1) / H.ty;
     H.full = s.pixels - (H.runs - 1) * H.ty;
-    H.inv_m = (float)(1.0 / ((double)s.pixels * H.cpg));
+    H.m = (float)((double)s.pixels * H.cpg);
     H.by_chunks = make_fast_div((uint32_t)H.chunks);
     H.by_tx = make_fast_div((uint32_t)H.tx);
     H.by_cpg = make_fast_div((uint32_t)H.cpg);

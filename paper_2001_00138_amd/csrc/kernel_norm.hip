@@ -1189,7 +1189,7 @@ Plan back_plan_of(const NormShape& s)
     // more constants a lane: fewer runs
     if (!held_of(s, v, p.one ? most : held_back_mixed_runs(bytes), true, p.H, p.threads, p.runs)) return p;
     p.room = p.runs <= 2 ? 2 : p.runs <= 4 ? 4 : p.runs <= 8 ? 8 : most;
-    if (!p.one && p.room > held_back_mixed_runs(bytes)) return p;          // no such kernel
+    if (!p.one && p.room > held_back_mixed_runs(bytes)) return p;          // no such kernel (nor does held_of ask for it)
     // (64 x 56x56x256 bf16, 32 bytes a pixel: 135 us held, 118 in two launches)
     if ((!p.H.folded && (s.pixels > 1024 || p.runs > 8)) || (p.H.chunk * bytes < 64 && (long long)s.n * p.H.chunks >= 256) ||
         held_back_lds(p.H, v, p.threads, held_in_lds(p.room), 16) > 160 * 1024)

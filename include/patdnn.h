@@ -459,6 +459,7 @@ patdnn_status_t patdnn_stack_run_static(patdnn_stack_t s, const float* input, fl
 #define PATDNN_F16   1     /* IEEE binary16 */
 #define PATDNN_BF16  2     /* bfloat16 */
 #define PATDNN_MXFP4 3     /* codes of patdnn_mxfp4_quantize, where a call says that it takes them */
+#define PATDNN_FP8   4     /* codes of patdnn_fp8_quantize with blocks along the rows, where a call says that it makes them */
 
 /* Activations. */
 #define PATDNN_ACT_NONE 0
@@ -555,6 +556,110 @@ size_t patdnn_mxfp4_linear_workspace_bytes(const patdnn_linear_desc_t* desc);
 patdnn_status_t patdnn_mxfp4_linear(const patdnn_linear_desc_t* desc, const void* x, const uint8_t* x_scales, const uint8_t* w,
                                     const uint8_t* w_scales, const float* bias, void* out, void* workspace,
                                     size_t workspace_bytes, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * The feed-forward half of a transformer's block, served or trained, in 8-bit floating point:
+ *   rms_norm (with the residual's addition) -> codes -> gated pair of projections -> codes -> linear
+ * and its gradients: linear, gated_backward, quantise, linear, rms_norm_backward.  The rules of the section above hold here too.
+ * ---------------------------------------------------------------------------------------------
+ */
+
+/*
+ * 8-bit floating point (e4m3: 4 bits of exponent, 3 of fraction, 448 the largest, no infinity) in blocks of 128 values that
+ * share a power of two.  A matrix [rows][cols] is stored in whole pieces of 128 columns, P = ceil(cols / 128):
+ *   codes   [rows][P * 128] bytes, zeros behind the last column.  16-byte aligned.
+ *   scales  a byte b for each block, which stands for 2^(b - 127):
+ *           PATDNN_FP8_ROWS     [rows][P]: blocks of 1 x 128 (activations, gradients)
+ *           PATDNN_FP8_SQUARES  [ceil(rows / 128)][P]: blocks of 128 x 128 (weights: the transpose's blocks are the same)
+ * Quantising: b - 127 is the smallest exponent, at least -127, with which the block's largest magnitude is at most 448 units (b = 0 for a
+ * block of zeros); a value becomes the nearest code to value / 2^(b - 127), ties to even.  A block that holds something
+ * not finite has b = 255 and zero codes; its values read back as NaN.  Powers of two are applied by the matrix instructions and are exact.
+ *   patdnn_fp8_quantize    x [rows][cols], `row` elements between rows (>= 0) -> its codes and scales; with `transposed` those of the
+ *       transpose, [cols][ceil(rows / 128) * 128]: what a product that sums over x's rows reads
+ *   patdnn_fp8_dequantize  the values [rows][cols] that codes and scales stand for, `row` elements between rows (>= cols)
+ * rows == 0 is a no-op (with `transposed` too).  PATDNN_EUNSUPPORTED beyond 2^24 workgroups of 2048 values in a launch (of 128 x 128, where
+ * blocks are squares or the matrix is transposed).
+ */
+#define PATDNN_FP8_ROWS    0
+#define PATDNN_FP8_SQUARES 1
+patdnn_status_t patdnn_fp8_quantize(const void* x, int32_t type, int32_t rows, int32_t cols, int64_t row, int32_t blocks, int32_t transposed,
+                                    uint8_t* codes, uint8_t* scales, void* stream);
+patdnn_status_t patdnn_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, int32_t rows, int32_t cols, int32_t blocks, void* out, int32_t type,
+                                      int64_t row, void* stream);
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition before it:
+ *   s = x + residual,  rstd = 1 / sqrt(mean of s^2 + eps),  y = gamma s rstd.
+ * Backward, with d = gamma dy, and s as the forward call stored it:
+ *   dx = dsum + rstd (d - s rstd^2 (mean of d s)),  dgamma = sum over rows of dy s rstd.
+ * dx is the gradient of s, so of x and of residual.
+ *   x, residual, sum   `type`; residual NULL: none; sum NULL: s is not stored.  sum may be residual itself (the same address and stride).
+ *   y                  `y_type`, or codes of patdnn_fp8_quantize (PATDNN_FP8, blocks along the rows) with y_scales; y_row is not read then.  y is made of
+ *                      s as it is in fp32, before it is rounded to `type`.
+ *   gamma              fp32 [cols], NULL for ones
+ *   rstd               fp32 [rows], output of the forward call (NULL: not wanted) and input of the backward one
+ *   dy                 `y_type` (no codes);  dsum, s, dx  `type`; dsum NULL: none.  dx may be dsum itself.
+ *   dgamma             fp32 [cols] or NULL; written, not added to (zeros for rows == 0)
+ *   workspace          patdnn_rms_norm_workspace_floats floats for the backward call with dgamma, contents undefined before and after
+ * Strides in elements between rows, values of a row adjacent (inputs >= 0, outputs >= cols).  Squares are added in fp32: a row with a mean square beyond its range
+ * has rstd 0.  Results repeat bit for bit.  rows == 0 is a no-op but for dgamma.  PATDNN_EUNSUPPORTED beyond 2^31 - 8321 columns and 2^24 workgroups (of a row, or of several short ones).
+ */
+typedef struct {
+    int32_t rows, cols;
+    int32_t type, y_type;
+    float eps;                      /* >= 0; not read by the backward call */
+    int64_t x_row;                  /* of x; of s in the backward call */
+    int64_t residual_row;           /* of residual; of dsum */
+    int64_t sum_row;                /* of sum; of dx */
+    int64_t y_row;                  /* of y; of dy */
+} patdnn_rms_desc_t;
+/* 0 for a description that the backward call would refuse. */
+size_t patdnn_rms_norm_workspace_floats(const patdnn_rms_desc_t* desc);
+patdnn_status_t patdnn_rms_norm(const patdnn_rms_desc_t* desc, const void* x, const void* residual, const float* gamma, void* sum, void* y,
+                                uint8_t* y_scales, float* rstd, void* stream);
+patdnn_status_t patdnn_rms_norm_backward(const patdnn_rms_desc_t* desc, const void* dy, const void* dsum, const void* s, const float* rstd,
+                                         const float* gamma, void* dx, float* dgamma, float* workspace, size_t workspace_floats, void* stream);
+
+/*
+ * Products of fp8 codes, summed in fp32.  x: codes [rows][in_features] with blocks along the rows.  Results in fp32 have fp32's precision; the others come
+ * from the fp8 matrix instruction, which cuts off what lies below 2^-13 of the largest of eight neighbouring products (1.5e-5 of a sum of normal values), and are faster.
+ *   patdnn_fp8_linear          out[m][n] = act(bias[n] + sum over k of x[m][k] w[n][k])
+ *   patdnn_fp8_gated           g = sum of x gate, u = sum of x up;  out = act(g) u
+ *   patdnn_fp8_gated_backward  from dh, the gradient of that result:  dgate = dh u act'(g),  dup = dh act(g)   (ReLU: act' is 0 where g <= 0); the
+ *                              projections are computed again.  The gradients of x and of the weights are products of these: quantised along
+ *                              out_features with the transposed weights' codes, and along rows with x's transposed codes.
+ *   w, gate, up   codes [out_features][in_features], all with scales of `w_blocks`.  PATDNN_FP8_ROWS also makes a product of two activations, or of a gradient
+ *                 and an activation.
+ *   bias          fp32 [out_features] or NULL
+ *   out, dgate, dup   `out_type`, `out_row` elements between rows; dgate and dup may be slices of one wider tensor.  patdnn_fp8_gated: codes too (PATDNN_FP8,
+ *                 blocks along the rows, with out_scales; out_row is not read then)
+ *   dh            `dh_type`, `dh_row` elements between rows (read by the backward call only)
+ *   workspace     the bytes that the call's own function names, 16-byte aligned (may be NULL if that is 0), contents undefined
+ *                 before and after; calls that share one must not overlap in time
+ * A block with scale 255 makes every sum that it is part of NaN.  Results repeat bit for bit.  rows == 0 is a no-op.  PATDNN_EUNSUPPORTED beyond 2^26 outputs, 2^31 - 257 rows,
+ * and where a launch would have more than some 2^22 workgroups.
+ */
+typedef struct {
+    int32_t rows, in_features, out_features;
+    int32_t w_blocks;               /* PATDNN_FP8_ROWS, _SQUARES */
+    int32_t out_type;
+    int32_t act;
+    int32_t dh_type;
+    int64_t out_row;                /* >= out_features */
+    int64_t dh_row;                 /* >= 0 */
+} patdnn_fp8_desc_t;
+size_t patdnn_fp8_linear_workspace_bytes(const patdnn_fp8_desc_t* desc);
+size_t patdnn_fp8_gated_workspace_bytes(const patdnn_fp8_desc_t* desc);
+size_t patdnn_fp8_gated_backward_workspace_bytes(const patdnn_fp8_desc_t* desc);
+patdnn_status_t patdnn_fp8_linear(const patdnn_fp8_desc_t* desc, const uint8_t* x, const uint8_t* x_scales, const uint8_t* w, const uint8_t* w_scales,
+                                  const float* bias, void* out, void* workspace, size_t workspace_bytes, void* stream);
+patdnn_status_t patdnn_fp8_gated(const patdnn_fp8_desc_t* desc, const uint8_t* x, const uint8_t* x_scales, const uint8_t* gate, const uint8_t* gate_scales,
+                                 const uint8_t* up, const uint8_t* up_scales, void* out, uint8_t* out_scales, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+patdnn_status_t patdnn_fp8_gated_backward(const patdnn_fp8_desc_t* desc, const void* dh, const uint8_t* x, const uint8_t* x_scales, const uint8_t* gate,
+                                          const uint8_t* gate_scales, const uint8_t* up, const uint8_t* up_scales, void* dgate, void* dup,
+                                          void* workspace, size_t workspace_bytes, void* stream);
 
 const char* patdnn_status_string(patdnn_status_t s);
 const char* patdnn_last_error(void);

@@ -32,9 +32,13 @@ EXPORTS = [
     "patdnn_channels_last", "patdnn_channels_first",
     "patdnn_group_norm", "patdnn_group_norm_backward", "patdnn_group_norm_workspace_floats",
     "patdnn_mxfp4_quantize", "patdnn_mxfp4_dequantize", "patdnn_mxfp4_linear", "patdnn_mxfp4_linear_workspace_bytes",
+    "patdnn_fp8_quantize", "patdnn_fp8_dequantize", "patdnn_rms_norm", "patdnn_rms_norm_backward", "patdnn_rms_norm_workspace_floats",
+    "patdnn_fp8_linear", "patdnn_fp8_linear_workspace_bytes", "patdnn_fp8_gated", "patdnn_fp8_gated_workspace_bytes",
+    "patdnn_fp8_gated_backward", "patdnn_fp8_gated_backward_workspace_bytes",
     "patdnn_status_string", "patdnn_last_error",
 ]
-PATDNN_F32, PATDNN_F16, PATDNN_BF16, PATDNN_MXFP4 = range(4)
+PATDNN_F32, PATDNN_F16, PATDNN_BF16, PATDNN_MXFP4, PATDNN_FP8 = range(5)
+FP8_BLOCKS = {"rows": 0, "squares": 1}
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
 
 
@@ -89,6 +93,18 @@ class LinearDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
                 ("x_type", ctypes.c_int32), ("out_type", ctypes.c_int32), ("act", ctypes.c_int32),
                 ("x_row", ctypes.c_int64), ("out_row", ctypes.c_int64)]
+
+
+class RmsDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("type", ctypes.c_int32), ("y_type", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("x_row", ctypes.c_int64), ("residual_row", ctypes.c_int64), ("sum_row", ctypes.c_int64),
+                ("y_row", ctypes.c_int64)]
+
+
+class Fp8Desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("w_blocks", ctypes.c_int32), ("out_type", ctypes.c_int32), ("act", ctypes.c_int32), ("dh_type", ctypes.c_int32),
+                ("out_row", ctypes.c_int64), ("dh_row", ctypes.c_int64)]
 
 
 class PatdnnError(RuntimeError):
@@ -155,6 +171,18 @@ def lib() -> ctypes.CDLL:
         L.patdnn_mxfp4_linear.argtypes = [ctypes.POINTER(LinearDesc), vp, vp, vp, vp, vp, vp, vp, size, vp]
         L.patdnn_mxfp4_linear_workspace_bytes.argtypes = [ctypes.POINTER(LinearDesc)]
         L.patdnn_mxfp4_linear_workspace_bytes.restype = size
+        L.patdnn_fp8_quantize.argtypes = [vp, i32, i32, i32, i64, i32, i32, vp, vp, vp]
+        L.patdnn_fp8_dequantize.argtypes = [vp, vp, i32, i32, i32, vp, i32, i64, vp]
+        L.patdnn_rms_norm.argtypes = [ctypes.POINTER(RmsDesc), vp, vp, vp, vp, vp, vp, vp, vp]
+        L.patdnn_rms_norm_backward.argtypes = [ctypes.POINTER(RmsDesc), vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.patdnn_rms_norm_workspace_floats.argtypes = [ctypes.POINTER(RmsDesc)]
+        L.patdnn_rms_norm_workspace_floats.restype = size
+        L.patdnn_fp8_linear.argtypes = [ctypes.POINTER(Fp8Desc), vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.patdnn_fp8_gated.argtypes = [ctypes.POINTER(Fp8Desc), vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.patdnn_fp8_gated_backward.argtypes = [ctypes.POINTER(Fp8Desc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        for name in ("linear", "gated", "gated_backward"):
+            getattr(L, f"patdnn_fp8_{name}_workspace_bytes").argtypes = [ctypes.POINTER(Fp8Desc)]
+            getattr(L, f"patdnn_fp8_{name}_workspace_bytes").restype = size
         L.patdnn_status_string.argtypes = [i32]
         L.patdnn_status_string.restype = ctypes.c_char_p
         L.patdnn_last_error.argtypes = []
@@ -747,6 +775,270 @@ def patdnn_group_norm_workspace_floats(n: int, pixels: int, channels: int, group
     image = pixels * channels
     desc = NormDesc(n, pixels, channels, groups, type, 0, 0.0, image, channels, image, channels, image, channels)
     return int(lib().patdnn_group_norm_workspace_floats(ctypes.byref(desc), int(bool(backward))))
+
+
+# ---------------------------------------------------------------------------
+# the feed-forward block in fp8: norm of rows, codes, linear layer, gated projections
+# ---------------------------------------------------------------------------
+
+def _call(like, stream, f, *args) -> None:
+    """f(*args, stream) with like's device current: without a stream its current one."""
+    torch = _torch()
+    index = like.device.index
+    if index == torch._C._cuda_getDevice():
+        _check(f(*args, _stream_ptr(stream)))
+    else:
+        with torch.cuda.device(index):
+            _check(f(*args, _stream_ptr(stream)))
+
+
+def _together(like, *tensors) -> None:
+    if not like.is_cuda:
+        raise ValueError("device tensor expected")
+    device = like.device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"all tensors must be on one device: {t.device} and {device}")
+
+
+def _typed_rows(t, shape, dtype, name: str) -> int:
+    """The row stride of a 2-d tensor that has to have this shape and type."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} of type {dtype}")
+    return _rows(t, name)
+
+
+def _byte_codes(t, name: str):
+    """Codes, as bytes or as torch's type of them."""
+    torch = _torch()
+    if t.dtype != torch.uint8 and t.dtype != torch.float8_e4m3fn:
+        raise ValueError(f"{name} must be uint8 or float8_e4m3fn")
+    if t.dim() != 2 or t.shape[1] == 0 or t.shape[1] % 128:
+        raise ValueError(f"{name} must be [rows, whole pieces of 128]")
+    return _devptr(t)
+
+
+def _byte_scales(t, rows: int, pieces: int, name: str, blocks=None):
+    """Scales of codes [rows, pieces * 128] -> (their pointer, how they are laid out; of one row both layouts are the same)."""
+    torch = _torch()
+    if t.dtype != torch.uint8 and t.dtype != torch.float8_e8m0fnu:
+        raise ValueError(f"{name} must be uint8 or float8_e8m0fnu")
+    shape = tuple(t.shape)
+    if shape == (rows, pieces) and blocks != 1:
+        return _devptr(t), 0
+    if shape == (-(-rows // 128), pieces) and blocks != 0:
+        return _devptr(t), 1
+    raise ValueError(f"{name} must be {(rows, pieces)}" + ("" if blocks == 0 else f" or {(-(-rows // 128), pieces)}"))
+
+
+def patdnn_fp8_quantize(x, codes=None, scales=None, *, blocks="rows", transposed=False, stream=None):
+    """x [rows, cols] -> (codes uint8 [rows, ceil(cols/128)*128], scales uint8): e4m3 with a power of two for each 1 x 128 (``blocks`` "rows", scales
+    [rows, ceil(cols/128)]) or 128 x 128 values ("squares", [ceil(rows/128), ceil(cols/128)]).  ``transposed``: those of x's transpose."""
+    torch = _torch()
+    try:
+        kind = FP8_BLOCKS[blocks]
+    except KeyError:
+        raise ValueError(f"blocks must be one of {', '.join(FP8_BLOCKS)}") from None
+    _together(x, codes, scales)
+    row = _rows(x, "x")
+    rows, cols = x.shape
+    r, c = (cols, rows) if transposed else (rows, cols)
+    pieces = -(-c // 128)
+    if codes is None:
+        codes = _new((r, pieces * 128), torch.uint8, x, stream)
+    elif tuple(codes.shape) != (r, pieces * 128):
+        raise ValueError(f"codes must be {(r, pieces * 128)}")
+    if scales is None:
+        scales = _new((-(-r // 128) if kind else r, pieces), torch.uint8, x, stream)
+    cp = _byte_codes(codes, "codes") if codes.numel() else _devptr(codes)
+    sp, _ = _byte_scales(scales, r, pieces, "scales", kind if r != 1 else None)
+    _call(x, stream, lib().patdnn_fp8_quantize, x.data_ptr(), _type(x.dtype), rows, cols, row, kind, int(bool(transposed)), cp, sp)
+    return codes, scales
+
+
+def patdnn_fp8_dequantize(codes, scales, cols: int, out=None, *, dtype=None, stream=None):
+    """The values [rows, cols] that codes and scales (of either layout) stand for, float32 unless ``out`` or ``dtype`` says otherwise."""
+    torch = _torch()
+    _together(codes, scales, out)
+    cp = _byte_codes(codes, "codes")
+    rows, pieces = codes.shape[0], codes.shape[1] // 128
+    if not 0 < cols <= pieces * 128 or cols <= (pieces - 1) * 128:
+        raise ValueError(f"{cols} columns are not {pieces} pieces of 128")
+    sp, kind = _byte_scales(scales, rows, pieces, "scales")
+    if out is None:
+        out = _new((rows, cols), dtype or torch.float32, codes, stream)
+    elif tuple(out.shape) != (rows, cols) or (dtype and out.dtype != dtype):
+        raise ValueError(f"output must be {(rows, cols)}, of type dtype if that is given")
+    _call(codes, stream, lib().patdnn_fp8_dequantize, cp, sp, rows, cols, kind, out.data_ptr(), _type(out.dtype), _rows(out, "output"))
+    return out
+
+
+def _row_floats(t, count: int, name: str, like, stream):
+    if t is None:
+        t = _new((count,), _torch().float32, like, stream)
+    return t, _float_vector(t, count, name)
+
+
+def patdnn_rms_norm(x, gamma=None, out=None, *, residual=None, sum=None, eps=1e-6, fp8=False, dtype=None, scales=None, rstd=None, stream=None):
+    """Root-mean-square norm of the rows of x [rows, cols] (+ ``residual``) -> (out, scales, sum, rstd).
+
+    gamma: float32 [cols] or None.  out: x's type, ``dtype``'s, or (``fp8``) the codes of patdnn_fp8_quantize, with their scales (None otherwise).
+    sum: x + residual in x's type, x itself without a residual; ``sum=residual`` adds in place.  rstd: float32 [rows], for the backward call."""
+    torch = _torch()
+    _together(x, gamma, out, residual, sum, scales, rstd)
+    x_row = _rows(x, "x")
+    rows, cols = x.shape
+    kind = _type(x.dtype)
+    residual_row = sum_row = 0
+    if residual is not None:
+        residual_row = _typed_rows(residual, x.shape, x.dtype, "residual")
+        if sum is None:
+            sum = _new((rows, cols), x.dtype, x, stream)
+    if sum is not None:
+        sum_row = _typed_rows(sum, x.shape, x.dtype, "sum")
+    if fp8:
+        pieces = -(-cols // 128)
+        if dtype is not None:
+            raise ValueError("dtype is for results that are no codes")
+        if out is None:
+            out = _new((rows, pieces * 128), torch.uint8, x, stream)
+        elif tuple(out.shape) != (rows, pieces * 128):
+            raise ValueError(f"output must be {(rows, pieces * 128)}")
+        if scales is None:
+            scales = _new((rows, pieces), torch.uint8, x, stream)
+        y_type, y_row, yp = PATDNN_FP8, 0, _byte_codes(out, "output")
+        sp, _ = _byte_scales(scales, rows, pieces, "scales", 0)
+    else:
+        if scales is not None:
+            raise ValueError("scales are for codes")
+        if out is None:
+            out = _new((rows, cols), dtype or x.dtype, x, stream)
+        elif out.shape != x.shape or (dtype and out.dtype != dtype):
+            raise ValueError("output must have the shape of x, and type dtype if that is given")
+        y_type, y_row, yp, sp = _type(out.dtype), _rows(out, "output"), out.data_ptr(), None
+    rstd, rp = _row_floats(rstd, rows, "rstd", x, stream)
+    desc = RmsDesc(rows, cols, kind, y_type, eps, x_row, residual_row, sum_row, y_row)
+    _call(x, stream, lib().patdnn_rms_norm, ctypes.byref(desc), x.data_ptr(), None if residual is None else residual.data_ptr(),
+          _float_vector(gamma, cols, "gamma"), None if sum is None else sum.data_ptr(), yp, sp, rp)
+    return out, scales, x if sum is None else sum, rstd
+
+
+def patdnn_rms_norm_backward(dy, sum, rstd, gamma=None, out=None, *, dsum=None, dgamma=None, workspace=None, stream=None):
+    """Gradients of patdnn_rms_norm: (dx like sum, dgamma float32 [cols]) from dy (of any type), the forward call's sum and rstd.  ``dsum``: the gradient that
+    arrives along the residual stream, added to dx; ``out=dsum`` adds in place."""
+    torch = _torch()
+    _together(sum, dy, rstd, gamma, out, dsum, dgamma, workspace)
+    s_row = _rows(sum, "sum")
+    rows, cols = sum.shape
+    if dy.shape != sum.shape:
+        raise ValueError("dy must have the shape of sum")
+    if out is None:
+        out = _new((rows, cols), sum.dtype, sum, stream)
+    desc = RmsDesc(rows, cols, _type(sum.dtype), _type(dy.dtype), 0.0, s_row, 0 if dsum is None else _typed_rows(dsum, sum.shape, sum.dtype, "dsum"),
+                   _typed_rows(out, sum.shape, sum.dtype, "output"), _rows(dy, "dy"))
+    dgamma, gp = _row_floats(dgamma, cols, "dgamma", sum, stream)
+    if workspace is None:
+        workspace = _new((lib().patdnn_rms_norm_workspace_floats(ctypes.byref(desc)),), torch.float32, sum, stream)
+    elif workspace.dtype != torch.float32:
+        raise ValueError("workspace must be a float32 tensor")
+    _call(sum, stream, lib().patdnn_rms_norm_backward, ctypes.byref(desc), dy.data_ptr(), None if dsum is None else dsum.data_ptr(), sum.data_ptr(),
+          _float_vector(rstd, rows, "rstd"), _float_vector(gamma, cols, "gamma"), out.data_ptr(), gp, _devptr(workspace), workspace.numel())
+    return out, dgamma
+
+
+def _fp8_operands(x, x_scales, weights):
+    """-> (rows, in_features, out_features, layout of the weights' scales, the pointers)"""
+    xp = _byte_codes(x, "x")
+    rows, cols = x.shape
+    pieces = cols // 128
+    sp, _ = _byte_scales(x_scales, rows, pieces, "x_scales", 0)
+    pointers, features, blocks = [xp, sp], None, None
+    for w, s in weights:
+        wp = _byte_codes(w, "weights")
+        if w.shape[1] != cols:
+            raise ValueError("the codes of x and of the weights must have rows of one length")
+        if features is None:
+            features = w.shape[0]
+        elif w.shape[0] != features:
+            raise ValueError("both projections must have the same number of outputs")
+        p, kind = _byte_scales(s, features, pieces, "scales of the weights", blocks)
+        blocks = kind
+        pointers += [wp, p]
+    return rows, cols, features, blocks, pointers
+
+
+def _byte_workspace(sizes, desc, workspace, like, stream):
+    """(workspace, its pointer, its bytes); allocated if it is needed and not given."""
+    if workspace is None:
+        needs = sizes(ctypes.byref(desc))
+        if not needs:
+            return None, None, 0
+        workspace = _new((needs,), _torch().uint8, like, stream)
+    return workspace, _devptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def patdnn_fp8_linear(x, x_scales, w, w_scales, bias=None, out=None, *, act="none", dtype=None, workspace=None, stream=None):
+    """fp8 codes x [rows, in] times codes w [out, in], plus bias (float32 [out]), activated.  The weights' scales are of rows or of squares, as their shape
+    says.  The result's type: ``out``'s or ``dtype``, float32 otherwise."""
+    torch = _torch()
+    _together(x, x_scales, w, w_scales, bias, out, workspace)
+    rows, cols, features, blocks, pointers = _fp8_operands(x, x_scales, ((w, w_scales),))
+    if out is None:
+        out = _new((rows, features), dtype or torch.float32, x, stream)
+    elif tuple(out.shape) != (rows, features) or (dtype and out.dtype != dtype):
+        raise ValueError(f"output must be {(rows, features)}, of type dtype if that is given")
+    desc = Fp8Desc(rows, cols, features, blocks, _type(out.dtype), _act(act), 0, _rows(out, "output"), 0)
+    workspace, wp, size = _byte_workspace(lib().patdnn_fp8_linear_workspace_bytes, desc, workspace, x, stream)
+    _call(x, stream, lib().patdnn_fp8_linear, ctypes.byref(desc), *pointers, _float_vector(bias, features, "bias"), out.data_ptr(), wp, size)
+    return out
+
+
+def patdnn_fp8_gated(x, x_scales, gate, gate_scales, up, up_scales, out=None, *, act="silu", fp8=False, dtype=None, scales=None, workspace=None,
+                     stream=None):
+    """act(x gate) * (x up) for fp8 codes x [rows, in] and gate, up [out, in]: values (of type ``out``'s or ``dtype``, float32 otherwise), or with
+    ``fp8`` (codes, scales) of patdnn_fp8_quantize."""
+    torch = _torch()
+    _together(x, x_scales, gate, gate_scales, up, up_scales, out, scales, workspace)
+    rows, cols, features, blocks, pointers = _fp8_operands(x, x_scales, ((gate, gate_scales), (up, up_scales)))
+    pieces = -(-features // 128)
+    shape = (rows, pieces * 128 if fp8 else features)
+    if fp8 and dtype is not None:
+        raise ValueError("dtype is for results that are no codes")
+    if not fp8 and scales is not None:
+        raise ValueError("scales are for codes")
+    if out is None:
+        out = _new(shape, torch.uint8 if fp8 else dtype or torch.float32, x, stream)
+    elif tuple(out.shape) != shape or (dtype and out.dtype != dtype):
+        raise ValueError(f"output must be {shape}, of type dtype if that is given")
+    if fp8:
+        if scales is None:
+            scales = _new((rows, pieces), torch.uint8, x, stream)
+        op, kind, row = _byte_codes(out, "output"), PATDNN_FP8, 0
+        sp, _ = _byte_scales(scales, rows, pieces, "scales", 0)
+    else:
+        op, kind, row, sp = out.data_ptr(), _type(out.dtype), _rows(out, "output"), None
+    desc = Fp8Desc(rows, cols, features, blocks, kind, _act(act), 0, row, 0)
+    workspace, wp, size = _byte_workspace(lib().patdnn_fp8_gated_workspace_bytes, desc, workspace, x, stream)
+    _call(x, stream, lib().patdnn_fp8_gated, ctypes.byref(desc), *pointers, op, sp, wp, size)
+    return (out, scales) if fp8 else out
+
+
+def patdnn_fp8_gated_backward(dh, x, x_scales, gate, gate_scales, up, up_scales, out=None, *, act="silu", dtype=None, workspace=None, stream=None):
+    """Gradients of the two projections of patdnn_fp8_gated from dh [rows, out], the gradient of its result: [rows, 2 * out], gate's beside up's, of type ``out``'s,
+    ``dtype`` or dh's."""
+    _together(x, x_scales, gate, gate_scales, up, up_scales, dh, out, workspace)
+    rows, cols, features, blocks, pointers = _fp8_operands(x, x_scales, ((gate, gate_scales), (up, up_scales)))
+    if tuple(dh.shape) != (rows, features):
+        raise ValueError(f"dh must be {(rows, features)}")
+    if out is None:
+        out = _new((rows, 2 * features), dtype or dh.dtype, x, stream)
+    elif tuple(out.shape) != (rows, 2 * features) or (dtype and out.dtype != dtype):
+        raise ValueError(f"output must be {(rows, 2 * features)}, of type dtype if that is given")
+    desc = Fp8Desc(rows, cols, features, blocks, _type(out.dtype), _act(act), _type(dh.dtype), _rows(out, "output"), _rows(dh, "dh"))
+    workspace, wp, size = _byte_workspace(lib().patdnn_fp8_gated_backward_workspace_bytes, desc, workspace, x, stream)
+    at = out.data_ptr()
+    _call(x, stream, lib().patdnn_fp8_gated_backward, ctypes.byref(desc), dh.data_ptr(), *pointers, at, at + features * out.element_size(), wp, size)
+    return out
 
 
 # ---------------------------------------------------------------------------

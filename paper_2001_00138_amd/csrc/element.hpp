@@ -8,7 +8,7 @@
 
 namespace patdnn {
 
-enum { kF32 = 0, kF16 = 1, kBF16 = 2, kMxfp4 = 3 };      // the PATDNN_F32... of patdnn.h
+enum { kF32 = 0, kF16 = 1, kBF16 = 2, kMxfp4 = 3, kFp8 = 4 };         // the PATDNN_F32... of patdnn.h
 enum { kActNone = 0, kActRelu = 1, kActSilu = 2 };       // the PATDNN_ACT_...
 
 inline size_t element_bytes(int type) { return type == kF32 ? 4 : 2; }

@@ -1,0 +1,49 @@
+// What the kernels of products of fp8 codes share.
+#pragma once
+
+#include "fp8.hpp"
+#include "linear.hpp"
+
+namespace patdnn {
+
+// Gradients of the two projections g and u from that of h = act(g) u.  SiLU's slope is s (1 + z (1 - s)) with s = 1 / (1 + exp(-z)), and 0
+// where s is.
+__device__ __forceinline__ void gated_gradients(float g, float u, float dh, int act, float& dg, float& du)
+{
+    float value = g, slope = 1.0f;
+    if (act == kActRelu) {
+        value = activate<kActRelu>(g);
+        slope = g <= 0.0f ? 0.0f : 1.0f;
+    } else if (act == kActSilu) {
+        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
+        value = g * s;
+        slope = s == 0.0f ? 0.0f : s * (1.0f + g * (1.0f - s));
+    }
+    dg = dh * u * slope;
+    du = dh * value;
+}
+__device__ __forceinline__ float load_as(const void* from, long long at, int type)
+{
+    return type == kF32 ? static_cast<const float*>(from)[at]
+           : type == kF16 ? static_cast<float>(static_cast<const _Float16*>(from)[at])
+                          : static_cast<float>(static_cast<const __bf16*>(from)[at]);
+}
+
+// One result: row m, column n.  a, b: its sums (b: of the second projection).
+template <int KIND>
+__device__ __forceinline__ void finish_one(const ProductShape& s, const ProductTensors& t, int m, int n, float a, float b)
+{
+    const long long at = m * s.out_row + n;
+    if (KIND == kLinear) {
+        store_as(t.out, at, s.out_type, activate_as(t.bias ? a + t.bias[n] : a, s.act));
+    } else if (KIND == kGated) {
+        store_as(t.out, at, s.out_type, activate_as(a, s.act) * b);
+    } else {
+        float dg, du;
+        gated_gradients(a, b, load_as(t.dh, m * s.dh_row + n, s.dh_type), s.act, dg, du);
+        store_as(t.out, at, s.out_type, dg);
+        store_as(t.out2, at, s.out_type, du);
+    }
+}
+
+}  // namespace patdnn

@@ -1,0 +1,136 @@
+// Products of fp8 codes, few rows of x: linear layers, and the gated pair of projections with its gradients.
+//
+// sum over k of x[m][k] w[n][k] on the scaled matrix instruction, which multiplies 16 rows of 128 codes with 16 others and applies the
+// scales of their blocks itself; sums are fp32.  (Results in fp32: bfloat16 instructions, a piece of 128 at a time, and its sums times their scales.)
+// The weights are the first operand, so that a lane's four results are neighbours along n.
+//
+// The weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs (of both projections); its wavefronts take
+// pieces of 128 values of k in turn, straight from memory to registers, and add their sums up in LDS, in their order.
+#include "fp8_products.hpp"
+
+namespace patdnn {
+
+namespace {
+
+constexpr int kRows = 16;                                // rows of x a workgroup
+constexpr int kAhead = 2;                                // pieces of weights that a wavefront asks for together
+
+struct Args {
+    ProductShape s;
+    ProductTensors t;
+    int pieces, row_tiles;                               // of 128 along k; of kRows rows of x
+    FastDiv by_tiles;
+};
+
+template <int KIND, bool EXACT>
+__global__ __launch_bounds__(1024) void product_rows_kernel(Args A)
+{
+    constexpr int kSides = KIND == kLinear ? 1 : 2;
+    extern __shared__ float sums[];                      // [wavefront][projection][lane][4]
+    // (the wavefront's number in a scalar register: a matrix instruction in a branch that only masks lanes out would be executed)
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = (int)blockDim.x >> 6;
+    const int r = lane & 15, kb = lane >> 4;
+    const uint32_t block = fast_div(blockIdx.x, A.by_tiles), m_tile = blockIdx.x - block * (uint32_t)A.row_tiles;
+    const int n0 = (int)block * 16, m0 = (int)m_tile * kRows, rows = min(kRows, A.s.rows - m0);
+    // rows past the end are read as the last one, and their results dropped
+    const long long n_row = min(n0 + r, A.s.out - 1), m_row = m0 + min(r, rows - 1);
+    const long long n_at = n_row * A.pieces * 128 + kb * 16, ns_at = (A.s.squares ? n_row >> 7 : n_row) * A.pieces;
+    const uint8_t* w_at[2] = {A.t.w + n_at, A.t.w2 + n_at};
+    const uint8_t* ws_at[2] = {A.t.w_scales + ns_at, A.t.w2_scales + ns_at};
+    const uint8_t* x_at = A.t.x + m_row * A.pieces * 128 + kb * 16;
+    const uint8_t* xs_at = A.t.x_scales + m_row * A.pieces;
+
+    auto load = [](const uint8_t* p) { return both_halves(*reinterpret_cast<const uint4*>(p), *reinterpret_cast<const uint4*>(p + 64)); };
+    floatx4 acc[kSides];
+#pragma unroll
+    for (int k = 0; k < kSides; ++k) acc[k] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int first = wave; first < A.pieces; first += kAhead * waves) {
+        int32x8 a[kAhead][kSides], b[kAhead];
+        uint32_t sa[kAhead][kSides], sb[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int piece = min(first + i * waves, A.pieces - 1);      // past the end: the last one, which is not multiplied
+#pragma unroll
+            for (int k = 0; k < kSides; ++k) {
+                a[i][k] = load(w_at[k] + piece * 128);
+                sa[i][k] = ws_at[k][piece];
+            }
+            b[i] = load(x_at + piece * 128);
+            sb[i] = xs_at[piece];
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (first + i * waves >= A.pieces) break;
+#pragma unroll
+            for (int k = 0; k < kSides; ++k) {
+                if constexpr (!EXACT) {
+                    acc[k] = fp8_multiply(a[i][k], b[i], acc[k], sa[i][k], sb[i]);
+                } else {
+                    const floatx4 z = fp8_multiply_exactly(a[i][k], b[i]);
+                    // the lane's results are of four of the weights' rows, whose scales lanes 4 kb ... hold
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[k][e] += z[e] * fp8_unit(sb[i]) * fp8_unit((uint32_t)__shfl((int)sa[i][k], kb * 4 + e, 64));
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kSides; ++k) *reinterpret_cast<floatx4*>(sums + ((wave * kSides + k) * 64 + lane) * 4) = acc[k];
+    __syncthreads();
+    for (int t = (int)threadIdx.x; t < rows * 16; t += (int)blockDim.x) {
+        const int nl = t & 15, ml = t >> 4, n = n0 + nl;
+        if (n >= A.s.out) continue;
+        const int at = ((nl >> 2) * 16 + ml) * 4 + (nl & 3);
+        float z[2] = {0.0f, 0.0f};
+        for (int i = 0; i < waves; ++i)
+#pragma unroll
+            for (int k = 0; k < kSides; ++k) z[k] += sums[(i * kSides + k) * 256 + at];
+        finish_one<KIND>(A.s, A.t, m0 + ml, n, z[0], z[1]);
+    }
+}
+
+long long workgroups_of(const ProductShape& s) { return (s.rows + kRows - 1ll) / kRows * ((s.out + 15ll) / 16); }
+
+template <int KIND, bool EXACT>
+hipError_t launch_rows(const ProductShape& s, const ProductTensors& t, hipStream_t stream)
+{
+    Args A{s, t, (int)fp8_pieces(s.in), (s.rows + kRows - 1) / kRows, {}};
+    A.by_tiles = make_fast_div((uint32_t)A.row_tiles);
+    const int waves = std::min(16, A.pieces);
+    hipLaunchKernelGGL((product_rows_kernel<KIND, EXACT>), dim3((unsigned)workgroups_of(s)), dim3((unsigned)waves * 64),
+                       (size_t)waves * (KIND == kLinear ? 1024 : 2048), stream, A);
+    return hipGetLastError();
+}
+
+// The workspace: h in fp32, where codes are made of it by a launch of their own.
+bool codes_apart(const ProductShape& s) { return s.kind == kGated && s.out_type == kFp8; }
+
+}  // namespace
+
+bool product_fits(const ProductShape& s)
+{
+    return fp8_pieces(s.in) * 128 <= INT32_MAX - 128 && s.rows <= INT32_MAX - 256 && ceil_div(s.out, 16) <= kMostBlocks / 4 &&
+           workgroups_of(s) <= kMostBlocks / 4 && (!codes_apart(s) || fp8_fits(Fp8Shape{s.rows, s.out, kF32, false, false, s.out}, true));
+}
+
+size_t product_workspace_bytes(const ProductShape& s) { return codes_apart(s) ? (size_t)s.rows * (size_t)s.out * 4 : 0; }
+
+hipError_t launch_product(const ProductShape& shape, const ProductTensors& tensors, void* workspace, hipStream_t stream)
+{
+    ProductShape s = shape;
+    ProductTensors t = tensors;
+    if (codes_apart(s)) {
+        s.out_type = kF32;
+        s.out_row = s.out;
+        t.out = workspace;
+    }
+    const bool exact = shape.out_type == kF32;
+    const hipError_t e = s.kind == kLinear  ? exact ? launch_rows<kLinear, true>(s, t, stream) : launch_rows<kLinear, false>(s, t, stream)
+                         : s.kind == kGated ? exact ? launch_rows<kGated, true>(s, t, stream) : launch_rows<kGated, false>(s, t, stream)
+                         : exact            ? launch_rows<kGatedBackward, true>(s, t, stream)
+                                            : launch_rows<kGatedBackward, false>(s, t, stream);
+    if (e != hipSuccess || !codes_apart(shape)) return e;
+    return launch_fp8_quantize(Fp8Shape{s.rows, s.out, kF32, false, false, s.out}, workspace, static_cast<uint8_t*>(tensors.out), tensors.out_scales, stream);
+}
+
+}  // namespace patdnn

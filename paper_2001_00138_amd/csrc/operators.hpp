@@ -1,4 +1,4 @@
-// Launchers of the operators around the pruned convolutions: order of channels, group norm, MXFP4.
+// Launchers of the operators around the pruned convolutions: order of channels, group norm, MXFP4, and the feed-forward block in fp8.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -60,5 +60,52 @@ bool linear_fits(const LinearShape& s);
 size_t linear_workspace_bytes(const LinearShape& s);
 hipError_t launch_linear(const LinearShape& s, const void* x, const uint8_t* x_scales, const uint8_t* w, const uint8_t* w_scales, const float* bias,
                          void* out, void* workspace, hipStream_t stream);
+
+// ---- fp8 (kernel_fp8.hip) ----
+// The stored matrix has `rows` x `cols` values; x is it, or (transposed) its transpose, with `row` elements between x's rows.
+struct Fp8Shape {
+    int rows, cols, type;
+    bool squares, transposed;
+    long long row;
+};
+inline long long fp8_pieces(long long cols) { return (cols + 127) / 128; }
+// Rows of scales of a stored matrix.
+inline long long fp8_scale_rows(long long rows, bool squares) { return squares ? (rows + 127) / 128 : rows; }
+bool fp8_fits(const Fp8Shape& s, bool quantize);
+hipError_t launch_fp8_quantize(const Fp8Shape& s, const void* x, uint8_t* codes, uint8_t* scales, hipStream_t stream);
+hipError_t launch_fp8_dequantize(const Fp8Shape& s, const uint8_t* codes, const uint8_t* scales, void* out, hipStream_t stream);
+
+// ---- root-mean-square norm (kernel_rms.hip) ----
+struct RmsShape {
+    int rows, cols, type, y_type;        // y_type: of y (kFp8: codes), or of dy
+    float eps;
+    long long x_row, residual_row, sum_row, y_row;       // backward: of s, dsum, dx, dy
+};
+bool rms_fits(const RmsShape& s, bool backward);
+size_t rms_workspace_floats(const RmsShape& s);          // of the backward call, for a gradient of gamma
+hipError_t launch_rms(const RmsShape& s, const void* x, const void* residual, const float* gamma, void* sum, void* y, uint8_t* y_scales,
+                      float* rstd, hipStream_t stream);
+hipError_t launch_rms_backward(const RmsShape& s, const void* dy, const void* dsum, const void* x, const float* rstd, const float* gamma, void* dx,
+                               float* dgamma, float* workspace, hipStream_t stream);
+
+// ---- products of fp8 codes (kernel_fp8_rows.hip, kernel_fp8_tiles.hip) ----
+enum { kLinear = 0, kGated = 1, kGatedBackward = 2 };
+struct ProductShape {
+    int kind;
+    int rows, in, out;                   // of x, along the sums, of the weights (of each of the two)
+    bool squares;                        // the weights' scales
+    int out_type, act, dh_type;
+    long long out_row, dh_row;
+};
+struct ProductTensors {
+    const uint8_t *x, *x_scales, *w, *w_scales, *w2, *w2_scales;         // w2: the second projection
+    const float* bias;
+    const void* dh;
+    void *out, *out2;                    // out2: the second projection's gradient
+    uint8_t* out_scales;                 // of codes
+};
+bool product_fits(const ProductShape& s);
+size_t product_workspace_bytes(const ProductShape& s);
+hipError_t launch_product(const ProductShape& s, const ProductTensors& t, void* workspace, hipStream_t stream);
 
 }  // namespace patdnn

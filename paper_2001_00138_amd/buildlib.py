@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libpatdnn.so")
 PROBES_LIB = os.path.join(HERE, "libpatdnn_probes.so")     # bench-side measurement probes
 SOURCES = ["patdnn_api.hip", "kernel_fkw.hip", "kernel_dw.hip", "kernel_compare.hip", "kernel_tiled.hip", "kernel_taps.hip", "kernel_f16.hip", "kernel_split.hip", "kernel_dense.hip", "selftest.hip",
            "kernel_reorder.hip", "kernel_norm.hip", "kernel_mxfp4.hip", "kernel_linear.hip", "kernel_linear_tiles.hip", "kernel_linear_short.hip",
-           "kernel_fp8.hip", "kernel_rms.hip", "kernel_fp8_rows.hip", "operators_api.hip", "encoder.cpp", "projection.cpp"]
+           "kernel_fp8.hip", "kernel_rms.hip", "kernel_fp8_rows.hip", "kernel_fp8_tiles.hip", "operators_api.hip", "encoder.cpp", "projection.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

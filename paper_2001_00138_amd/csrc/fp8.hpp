@@ -76,20 +76,29 @@ __device__ __forceinline__ floatx4 fp8_multiply(const int32x8& a, const int32x8&
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, BYTE, (int)scale_a, BYTE, (int)scale_b);
 }
-// Eight codes in bfloat16, which holds them exactly.
+// The same for results in fp32, at half the rate: codes become bfloat16, multiplied by their scales on the way, and go through four bfloat16
+// instructions, whose products and sums are fp32's.  Exact but for values below 2^-126, which have bfloat16's subnormals left; a scale of NaN makes
+// NaN of any code.  unit: the scale's byte where a float's exponent is.
 typedef __bf16 bfloatx8 __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ bfloatx8 fp8_widen(int low, int high)
+struct Wide {
+    bfloatx8 v[4];
+};
+__device__ __forceinline__ Wide fp8_widen(const int32x8& a, uint32_t unit)
 {
-    const bfloatx2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)low, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)low, 1.0f, true);
-    const bfloatx2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)high, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)high, 1.0f, true);
-    return bfloatx8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-// The same product without the scales, for results in fp32, through four bfloat16 instructions (half the rate), whose products and sums are fp32's.
-__device__ __forceinline__ floatx4 fp8_multiply_exactly(const int32x8& a, const int32x8& b)
-{
-    floatx4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float s = __uint_as_float(unit);
+    Wide w;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_widen(a[i], a[i + 1]), fp8_widen(b[i], b[i + 1]), c, 0, 0, 0);
+    for (int i = 0; i < 4; ++i) {
+        const bfloatx2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)a[2 * i], s, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)a[2 * i], s, true);
+        const bfloatx2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)a[2 * i + 1], s, false), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)a[2 * i + 1], s, true);
+        w.v[i] = bfloatx8{p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
+    }
+    return w;
+}
+__device__ __forceinline__ floatx4 multiply_wide(const Wide& a, const Wide& b, floatx4 c)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], c, 0, 0, 0);
     return c;
 }
 __device__ __forceinline__ int32x8 both_halves(const uint4& a, const uint4& b)

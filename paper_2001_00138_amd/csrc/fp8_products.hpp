@@ -46,4 +46,27 @@ __device__ __forceinline__ void finish_one(const ProductShape& s, const ProductT
     }
 }
 
+// Sixteen neighbouring values of a row, `left` of them inside it.
+template <class T>
+__device__ __forceinline__ void load_sixteen(const void* from, long long at, int left, float (&z)[16])
+{
+#pragma unroll
+    for (int i = 0; i < 16; i += 8) {
+        float v[8];
+        load8_floats(static_cast<const T*>(from) + at + i, left - i, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[i + e] = v[e];
+    }
+}
+__device__ __forceinline__ void load_values(const void* from, long long at, int type, int left, float (&z)[16])
+{
+    if (type == kF32) load_sixteen<float>(from, at, left, z);
+    else if (type == kF16) load_sixteen<_Float16>(from, at, left, z);
+    else load_sixteen<__bf16>(from, at, left, z);
+}
+
+// Many rows (kernel_fp8_tiles.hip).
+bool product_tiles_fit(const ProductShape& s);
+hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, hipStream_t stream);
+
 }  // namespace patdnn

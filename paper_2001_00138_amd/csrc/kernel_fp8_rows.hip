@@ -1,7 +1,7 @@
 // Products of fp8 codes, few rows of x: linear layers, and the gated pair of projections with its gradients.
 //
 // sum over k of x[m][k] w[n][k] on the scaled matrix instruction, which multiplies 16 rows of 128 codes with 16 others and applies the
-// scales of their blocks itself; sums are fp32.  (Results in fp32: bfloat16 instructions, a piece of 128 at a time, and its sums times their scales.)
+// scales of their blocks itself; sums are fp32.  (Results in fp32: bfloat16 instructions.)
 // The weights are the first operand, so that a lane's four results are neighbours along n.
 //
 // The weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs (of both projections); its wavefronts take
@@ -63,14 +63,8 @@ __global__ __launch_bounds__(1024) void product_rows_kernel(Args A)
             if (first + i * waves >= A.pieces) break;
 #pragma unroll
             for (int k = 0; k < kSides; ++k) {
-                if constexpr (!EXACT) {
-                    acc[k] = fp8_multiply(a[i][k], b[i], acc[k], sa[i][k], sb[i]);
-                } else {
-                    const floatx4 z = fp8_multiply_exactly(a[i][k], b[i]);
-                    // the lane's results are of four of the weights' rows, whose scales lanes 4 kb ... hold
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[k][e] += z[e] * fp8_unit(sb[i]) * fp8_unit((uint32_t)__shfl((int)sa[i][k], kb * 4 + e, 64));
-                }
+                if constexpr (EXACT) acc[k] = multiply_wide(fp8_widen(a[i][k], sa[i][k] << 23), fp8_widen(b[i], sb[i] << 23), acc[k]);
+                else acc[k] = fp8_multiply(a[i][k], b[i], acc[k], sa[i][k], sb[i]);
             }
         }
     }
@@ -102,34 +96,39 @@ hipError_t launch_rows(const ProductShape& s, const ProductTensors& t, hipStream
     return hipGetLastError();
 }
 
+// Whether the call is for this kernel and not for tiles.
+bool by_rows(const ProductShape& s) { return s.rows <= kRows || !product_tiles_fit(s); }
+
 // The workspace: h in fp32, where codes are made of it by a launch of their own.
-bool codes_apart(const ProductShape& s) { return s.kind == kGated && s.out_type == kFp8; }
+bool codes_apart(const ProductShape& s) { return s.kind == kGated && s.out_type == kFp8 && by_rows(s); }
 
 }  // namespace
 
 bool product_fits(const ProductShape& s)
 {
     return fp8_pieces(s.in) * 128 <= INT32_MAX - 128 && s.rows <= INT32_MAX - 256 && ceil_div(s.out, 16) <= kMostBlocks / 4 &&
-           workgroups_of(s) <= kMostBlocks / 4 && (!codes_apart(s) || fp8_fits(Fp8Shape{s.rows, s.out, kF32, false, false, s.out}, true));
+           (!by_rows(s) || workgroups_of(s) <= kMostBlocks / 4) &&
+           (!codes_apart(s) || fp8_fits(Fp8Shape{s.rows, s.out, kF32, false, false, s.out}, true));
 }
 
 size_t product_workspace_bytes(const ProductShape& s) { return codes_apart(s) ? (size_t)s.rows * (size_t)s.out * 4 : 0; }
 
 hipError_t launch_product(const ProductShape& shape, const ProductTensors& tensors, void* workspace, hipStream_t stream)
 {
+    if (!by_rows(shape)) return launch_product_tiles(shape, tensors, stream);
     ProductShape s = shape;
     ProductTensors t = tensors;
-    if (codes_apart(s)) {
+    const bool apart = codes_apart(s), exact = s.out_type == kF32;
+    if (apart) {
         s.out_type = kF32;
         s.out_row = s.out;
         t.out = workspace;
     }
-    const bool exact = shape.out_type == kF32;
     const hipError_t e = s.kind == kLinear  ? exact ? launch_rows<kLinear, true>(s, t, stream) : launch_rows<kLinear, false>(s, t, stream)
                          : s.kind == kGated ? exact ? launch_rows<kGated, true>(s, t, stream) : launch_rows<kGated, false>(s, t, stream)
                          : exact            ? launch_rows<kGatedBackward, true>(s, t, stream)
                                             : launch_rows<kGatedBackward, false>(s, t, stream);
-    if (e != hipSuccess || !codes_apart(shape)) return e;
+    if (e != hipSuccess || !apart) return e;
     return launch_fp8_quantize(Fp8Shape{s.rows, s.out, kF32, false, false, s.out}, workspace, static_cast<uint8_t*>(tensors.out), tensors.out_scales, stream);
 }
 

@@ -1,0 +1,365 @@
+// Products of fp8 codes, many rows of x: tiles of BN of the weights' rows x BM rows of x, both operands through LDS.
+//
+// A workgroup walks k in stages of 128 codes.  NS stages are in LDS, and arrive straight from memory.  A wavefront holds a stage's operands in two halves each;
+// it multiplies them in an order that turns round from stage to stage, so that each half is read from LDS while another two are multiplied
+// and none is held twice.  Half-way through a stage everything of it is in registers: there the workgroup meets, the stage's place in LDS is
+// given to the stage NS ahead, and reading the next one begins under the second half of the products.
+//
+// LDS holds 16-byte chunks, eight a row; a chunk of a row stands at its place xor a number that depends on the row, chosen so that the eight lanes
+// that are served in one cycle find theirs in different banks.  The weights' rows of a wavefront are dealt to the instruction's rows so that a lane's
+// results for four tiles are sixteen neighbouring outputs.  For the gated pair, each 64 rows of the first projection's are followed by the same 64 of the second's,
+// so that one lane has both sums of an output, and a workgroup all 128 outputs that share a scale.
+#include "fp8_products.hpp"
+
+namespace patdnn {
+
+namespace {
+
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
+struct Args {
+    ProductShape s;
+    ProductTensors t;
+    int pieces;                                          // stages
+    int tiles_n, tiles_m;
+    FastDiv by_band, by_last;                            // tiles of a band, rows of tiles of the last band
+};
+constexpr int kBand = 8;                                 // rows of tiles that are taken side by side
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Moves 16 bytes a lane from memory to LDS: lane l's to lds + 16 l, the start from m0, which the compiler keeps for itself and finds as it
+// was (the load reads it as it is issued).  Not waited for: s_waitcnt vmcnt counts it.
+__device__ __forceinline__ void fetch16(intx4 buffer, uint32_t lds, uint32_t lane_offset, uint32_t offset)
+{
+    uint32_t kept;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(lds), "v"(lane_offset), "s"(buffer), "s"(offset) : "memory");
+}
+template <int OUTSTANDING>
+__device__ __forceinline__ void wait_fetches()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OUTSTANDING) : "memory");
+}
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ __forceinline__ intx4 buffer_of(const void* p)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return intx4{uniform((int)(uint32_t)a), uniform((int)(uint32_t)(a >> 32) & 0xffff), -1, 0x00020000};
+}
+
+// BN x BM rows of the weights and of x, on WN x WM wavefronts, NS stages in LDS.
+template <int BN, int BM, int WN, int WM, int NS>
+struct Tile {
+    static constexpr int kWaves = WN * WM, kThreads = 64 * kWaves, kRows = BN + BM;
+    static constexpr int kTN = BN / WN / 16, kTM = BM / WM / 16;         // matrix tiles of a wavefront
+    static constexpr int kHN = kTN / 2, kHM = kTM > 1 ? kTM / 2 : 1;     // of a half
+    static constexpr int kFetches = kRows / 8 / kWaves;                  // of 8 rows, per wavefront and stage
+    static constexpr int kStage = kRows * 128, kScales = NS * kStage, kLds = kScales + kRows * 4;
+    static_assert(kTN % 4 == 0 && (kTM == 1 || kTM % 2 == 0) && kRows % (8 * kWaves) == 0 && BN % 64 == 0 && BM % 16 == 0 && kRows <= kThreads, "shape");
+    static_assert(NS == 2 || NS == 4, "stages by their place in a group of four");
+};
+
+template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS>
+__global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
+{
+    using S = Tile<BN, BM, WN, WM, NS>;
+    constexpr bool kTwo = KIND != kLinear;
+    constexpr int kOut = kTwo ? BN / 2 : BN;                             // outputs of a workgroup
+    static_assert(!kTwo || S::kTN == 8, "a wavefront has 64 rows of each projection");
+    extern __shared__ char lds[];
+    const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    const int r = lane & 15, kb = lane >> 4;
+    // Which tile: workgroups go to the eight XCDs in turn, each takes a run of tiles, kBand rows of them at a time.
+    int tn, tm;
+    {
+        const int all = A.tiles_n * A.tiles_m, xcd = (int)blockIdx.x & 7, q = all >> 3, rest = all & 7;
+        const int t = xcd * q + min(xcd, rest) + ((int)blockIdx.x >> 3);
+        const int band = uniform((int)fast_div((uint32_t)t, A.by_band)), in_band = t - band * kBand * A.tiles_n, height = min(kBand, A.tiles_m - band * kBand);
+        tn = uniform(height == kBand ? in_band / kBand : (int)fast_div((uint32_t)in_band, A.by_last));
+        tm = band * kBand + in_band - tn * height;
+    }
+    const int n0 = tn * kOut, m0 = tm * BM, pieces = A.pieces;
+    const long long pitch = (long long)pieces * 128;
+
+    // A row of LDS: whose it is (0, 1: of the weights; 2: of x), and which row behind the tile's first.  Rows past the end are those of the last one.
+    auto side_of = [&](int row) { return row >= BN ? 2 : kTwo ? row >> 6 & 1 : 0; };
+    auto row_of = [&](int row) { return row >= BN ? row - BN : kTwo ? (row >> 7) * 64 + (row & 63) : row; };
+    const int w_last = A.s.out - 1 - n0, x_last = A.s.rows - 1 - m0;
+    const intx4 from_w = buffer_of(A.t.w + n0 * pitch), from_w2 = buffer_of(kTwo ? A.t.w2 + n0 * pitch : A.t.w), from_x = buffer_of(A.t.x + m0 * pitch);
+    const int fetch_row = wave * S::kFetches * 8;                        // this wavefront's first row
+    uint32_t data_at[S::kFetches];
+#pragma unroll
+    for (int i = 0; i < S::kFetches; ++i) {
+        const int first = fetch_row + i * 8, row = first + (lane >> 3);
+        const int swap = first < BN ? (row & 3) | (row >> 4 & 1) << 2 : row & 7;
+        data_at[i] = (uint32_t)(min(row_of(row), first < BN ? w_last : x_last) * (int)pitch) + (uint32_t)(((lane & 7) ^ swap) * 16);
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    auto fetch_stage = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < S::kFetches; ++i) {
+            const int first = fetch_row + i * 8, side = side_of(first);
+            fetch16(side == 2 ? from_x : kTwo && side == 1 ? from_w2 : from_w, lds0 + (uint32_t)((t & (NS - 1)) * S::kStage + first * 128), data_at[i], (uint32_t)t * 128);
+        }
+    };
+    // Scales of a group of four stages, a word for each row of LDS: in a register until the group before is done with LDS's.
+    const uint8_t* scales_at;
+    bool has_scales = (int)threadIdx.x < S::kRows;
+    {
+        const int row = (int)threadIdx.x, side = side_of(row);
+        const uint8_t* from = side == 2 ? A.t.x_scales : kTwo && side == 1 ? A.t.w2_scales : A.t.w_scales;
+        const int at = side == 2 ? m0 + min(row_of(row), x_last) : n0 + min(row_of(row), w_last);
+        scales_at = from + (long long)(side != 2 && A.s.squares ? at >> 7 : at) * pieces;
+    }
+    uint32_t word = 0;
+    auto fetch_scales = [&](int t) {
+        if (!has_scales) return;
+        if (t + 4 <= pieces) {
+            word = __builtin_bit_cast(uint32_t, load_pack<uint8_t, 4>(scales_at + t));
+        } else {
+            word = 0;
+            for (int i = 0; i < pieces - t; ++i) word |= (uint32_t)scales_at[t + i] << (8 * i);
+        }
+    };
+    auto put_scales = [&]() {
+        if (has_scales) *reinterpret_cast<uint32_t*>(lds + S::kScales + (int)threadIdx.x * 4) = word;
+    };
+
+    const int wn = wave % WN, wm = wave / WN;
+    const int a_row = wn * (16 * S::kTN) + (r >> 2) * 16 + (r & 3), b_row = BN + wm * (16 * S::kTM) + r;
+    const int a_at = a_row * 128 + (kb ^ ((r & 3) | (r >> 2 & 1) << 2)) * 16, b_at = b_row * 128 + (kb ^ (r & 7)) * 16;
+    auto chunks = [&](int at) {
+        return both_halves(*reinterpret_cast<const uint4*>(lds + at), *reinterpret_cast<const uint4*>(lds + (at ^ 64)));
+    };
+
+    floatx4 acc[S::kTN][S::kTM];
+#pragma unroll
+    for (int i = 0; i < S::kTN; ++i)
+#pragma unroll
+        for (int j = 0; j < S::kTM; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t sa[S::kTN], sb[S::kTM];
+    int32x8 a[2][S::kHN], b[2][S::kHM];                  // halves; of a single tile of x: two stages
+    auto read_a = [&](int buffer, int half) {
+#pragma unroll
+        for (int i = 0; i < S::kHN; ++i) {
+            const int tile = half * S::kHN + i;
+            a[half][i] = chunks(buffer * S::kStage + a_at + ((tile >> 2) * 64 + (tile & 3) * 4) * 128);
+        }
+    };
+    auto read_b = [&](int buffer, int half) {
+#pragma unroll
+        for (int j = 0; j < S::kHM; ++j) b[half][j] = chunks(buffer * S::kStage + b_at + (S::kTM > 1 ? half * S::kHM + j : 0) * 16 * 128);
+    };
+
+    fetch_scales(0);
+    for (int t = 0; t < min(NS, pieces); ++t) fetch_stage(t);
+    put_scales();
+    wait_fetches<0>();
+    meet();
+    read_a(0, 0);
+    read_b(0, 0);
+
+    auto stage = [&](auto step, int t) {
+        constexpr int STEP = decltype(step)::value, F = STEP & 1, HERE = STEP & (NS - 1), NEXT = (STEP + 1) & (NS - 1);
+        if (STEP == 0) {
+#pragma unroll
+            for (int i = 0; i < S::kTN; ++i)
+                sa[i] = *reinterpret_cast<const uint32_t*>(lds + S::kScales + (a_row + (i >> 2) * 64 + (i & 3) * 4) * 4);
+#pragma unroll
+            for (int j = 0; j < S::kTM; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(lds + S::kScales + (b_row + j * 16) * 4);
+            if (t + 4 < pieces) fetch_scales(t + 4);
+        }
+        auto multiply = [&](int ha, int hb) {
+#pragma unroll
+            for (int i = 0; i < S::kHN; ++i)
+#pragma unroll
+                for (int j = 0; j < S::kHM; ++j) {
+                    const int n = ha * S::kHN + i, m = (S::kTM > 1 ? hb * S::kHM : 0) + j;
+                    acc[n][m] = fp8_multiply<STEP>(a[ha][i], b[hb][j], acc[n][m], sa[n], sb[m]);
+                }
+        };
+        // (in bfloat16 a tile of x is made once a stage, one of the weights where it is multiplied with all of x's)
+        Wide wide[EXACT ? S::kTM : 1];
+        auto widen_b = [&](int hb) {
+#pragma unroll
+            for (int j = 0; j < S::kHM; ++j) {
+                const int m = (S::kTM > 1 ? hb * S::kHM : 0) + j;
+                wide[EXACT ? m : 0] = fp8_widen(b[hb][j], (sb[m] >> (8 * STEP) & 255) << 23);
+            }
+        };
+        auto multiply_half = [&](int ha) {
+#pragma unroll
+            for (int i = 0; i < S::kHN; ++i) {
+                const int n = ha * S::kHN + i;
+                const Wide w = fp8_widen(a[ha][i], (sa[n] >> (8 * STEP) & 255) << 23);
+#pragma unroll
+                for (int m = 0; m < S::kTM; ++m) acc[n][m] = multiply_wide(w, wide[EXACT ? m : 0], acc[n][m]);
+            }
+        };
+        if (S::kTM > 1) read_b(HERE, F ^ 1);
+        if constexpr (EXACT) {
+            read_a(HERE, 1);
+            widen_b(F);
+            if (S::kTM > 1) widen_b(F ^ 1);
+            multiply_half(0);
+        } else {
+            multiply(0, F);
+            read_a(HERE, 1);
+            if (S::kTM > 1) multiply(0, F ^ 1);
+        }
+        if (t + 1 < pieces) {
+            // the next stage has arrived once no more than those behind it are on their way
+            if (NS > 2 && t + NS <= pieces) wait_fetches<(NS - 2) * S::kFetches>();
+            else wait_fetches<0>();
+            if (STEP == 3) put_scales();
+            meet();
+            if (t + NS < pieces) fetch_stage(t + NS);
+            read_a(NEXT, 0);
+        }
+        if constexpr (EXACT) {
+            multiply_half(1);
+            if (t + 1 < pieces) read_b(NEXT, F ^ 1);
+        } else {
+            if (S::kTM > 1) multiply(1, F ^ 1);
+            if (t + 1 < pieces) read_b(NEXT, F ^ 1);
+            multiply(1, F);
+        }
+    };
+    for (int t = 0; t < pieces; t += 4) {
+        stage(Const<0>{}, t);
+        if (t + 1 < pieces) stage(Const<1>{}, t + 1);
+        if (t + 2 < pieces) stage(Const<2>{}, t + 2);
+        if (t + 3 < pieces) stage(Const<3>{}, t + 3);
+    }
+
+    // A lane's results: row m0 + ... + r of x, sixteen neighbouring outputs for each four tiles (and their other sums four tiles on).
+    constexpr int kGroups = kTwo ? 1 : S::kTN / 4;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const int n = n0 + wn * (kOut / WN) + g * 64 + kb * 16, left = A.s.out - n;
+        float add[16];
+        if (KIND == kLinear)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) add[i] = A.t.bias && i < left ? A.t.bias[n + i] : 0.0f;
+        if (KIND == kGated && A.s.out_type == kFp8) {
+            // the largest of a row's 128 outputs is that of its lanes in the two wavefronts that have them
+            static_assert(!kTwo || WN == 2, "128 outputs in two wavefronts");
+            uint32_t* tops = reinterpret_cast<uint32_t*>(lds);           // [wn][row]
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < S::kTM; ++j) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float h = i < left ? activate_as(acc[g * 4 + i / 4][j][i % 4], A.s.act) * acc[(g + (kTwo ? 1 : 0)) * 4 + i / 4][j][i % 4] : 0.0f;
+                    acc[g * 4 + i / 4][j][i % 4] = h;
+                    top = max(top, __float_as_uint(h) & 0x7fffffffu);
+                }
+                top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+                top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+                if (kb == 0) tops[wn * BM + wm * (16 * S::kTM) + j * 16 + r] = top;
+            }
+            __syncthreads();
+            const int out_pieces = (A.s.out + 127) / 128;
+#pragma unroll
+            for (int j = 0; j < S::kTM; ++j) {
+                const int at = wm * (16 * S::kTM) + j * 16 + r, m = m0 + at;
+                if (m >= A.s.rows) continue;
+                const uint32_t byte = fp8_scale_byte(max(tops[at], tops[BM + at]));
+                const float inverse = fp8_inverse(byte);
+                uint32_t c[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const floatx4 h = acc[g * 4 + i][j];
+                    c[i] = byte == kNanScale ? 0u : fp8_encode4(h[0], h[1], h[2], h[3], inverse);
+                }
+                *reinterpret_cast<uint4*>(static_cast<uint8_t*>(A.t.out) + ((long long)m * out_pieces + tn) * 128 + wn * 64 + kb * 16) =
+                    make_uint4(c[0], c[1], c[2], c[3]);
+                if (wn == 0 && kb == 0) A.t.out_scales[(long long)m * out_pieces + tn] = (uint8_t)byte;
+            }
+            continue;
+        }
+#pragma unroll
+        for (int j = 0; j < S::kTM; ++j) {
+            const int m = m0 + wm * (16 * S::kTM) + j * 16 + r;
+            if (m >= A.s.rows || left <= 0) continue;
+            float z[16], y[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = acc[g * 4 + i / 4][j][i % 4];
+            const long long at = m * A.s.out_row + n;
+            if (KIND == kLinear) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] += add[i];
+                finish_sixteen(z, A.s.act);
+                store_results(A.t.out, at, A.s.out_type, left, z);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = acc[(g + (kTwo ? 1 : 0)) * 4 + i / 4][j][i % 4];
+                if (KIND == kGated) {
+                    finish_sixteen(z, A.s.act);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] *= y[i];
+                    store_results(A.t.out, at, A.s.out_type, left, z);
+                } else {
+                    float d[16];
+                    load_values(A.t.dh, m * A.s.dh_row + n, A.s.dh_type, left, d);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float gate = z[i], up = y[i];
+                        gated_gradients(gate, up, d[i], A.s.act, z[i], y[i]);
+                    }
+                    store_results(A.t.out, at, A.s.out_type, left, z);
+                    store_results(A.t.out2, at, A.s.out_type, left, y);
+                }
+            }
+        }
+    }
+}
+
+template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS>
+hipError_t launch_shape(Args A, hipStream_t stream)
+{
+    using S = Tile<BN, BM, WN, WM, NS>;
+    constexpr int kOut = KIND == kLinear ? BN : BN / 2;
+    A.tiles_n = (A.s.out + kOut - 1) / kOut;
+    A.tiles_m = (A.s.rows + BM - 1) / BM;
+    A.by_band = make_fast_div((uint32_t)(kBand * A.tiles_n));
+    A.by_last = make_fast_div((uint32_t)(A.tiles_m % kBand ? A.tiles_m % kBand : kBand));
+    static std::atomic<uint64_t> allowed{0};
+    const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS>), allowed);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS>), dim3((unsigned)(A.tiles_n * A.tiles_m)), dim3(S::kThreads), S::kLds, stream, A);
+    return hipGetLastError();
+}
+
+// Rows of x a tile: the largest that give every CU one.
+long long tiles_of(const ProductShape& s, int bn, int bm) { return ceil_div(s.out, bn) * ceil_div(s.rows, bm); }
+
+}  // namespace
+
+bool product_tiles_fit(const ProductShape& s)
+{
+    // offsets in a tile are 32-bit; the smallest tiles are 64 x 64
+    return fp8_pieces(s.in) * 128 * 256 <= INT32_MAX && tiles_of(s, 64, 64) <= kMostBlocks / 4;
+}
+
+hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, hipStream_t stream)
+{
+    Args A{s, t, (int)fp8_pieces(s.in), 0, 0, {}, {}};
+    const bool exact = s.out_type == kF32;
+    if (s.kind == kLinear) {
+        if (exact) return tiles_of(s, 128, 128) >= 256 ? launch_shape<kLinear, true, 128, 128, 2, 2, 2>(A, stream) : launch_shape<kLinear, true, 64, 64, 1, 4, 2>(A, stream);
+        return tiles_of(s, 256, 256) >= 256   ? launch_shape<kLinear, false, 256, 256, 2, 4, 2>(A, stream)
+               : tiles_of(s, 128, 128) >= 256 ? launch_shape<kLinear, false, 128, 128, 2, 2, 2>(A, stream)
+                                              : launch_shape<kLinear, false, 64, 64, 1, 4, 4>(A, stream);
+    }
+    auto run = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        if (exact) return tiles_of(s, 128, 128) >= 256 ? launch_shape<KIND, true, 256, 128, 2, 4, 2>(A, stream) : launch_shape<KIND, true, 256, 64, 2, 4, 2>(A, stream);
+        return tiles_of(s, 128, 256) >= 256 ? launch_shape<KIND, false, 256, 256, 2, 4, 2>(A, stream) : launch_shape<KIND, false, 256, 64, 2, 4, 2>(A, stream);
+    };
+    return s.kind == kGated ? run(Const<kGated>{}) : run(Const<kGatedBackward>{});
+}
+
+}  // namespace patdnn

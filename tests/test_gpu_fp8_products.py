@@ -202,3 +202,51 @@ def test_graph_and_no_rows(torch):
     assert B.patdnn_fp8_linear(xc[:0], xs[:0], gc, gs).shape == (0, 200)
     assert B.patdnn_fp8_gated(xc[:0], xs[:0], gc, gs, uc, us, fp8=True)[0].shape == (0, 256)
     assert B.patdnn_fp8_gated_backward(x[:0, :200], xc[:0], xs[:0], gc, gs, uc, us).shape == (0, 400)
+
+
+# (sizes that take each tile shape, with rows and outputs that end inside a tile, and k of one to nine stages)
+LARGE = [(4090, 300, 4100), (2100, 520, 2000), (520, 1100, 700), (8200, 128, 2050), (300, 1030, 33000)]
+
+
+def whole(torch, rows, k, squares, seed):
+    """Codes of whole numbers up to 15, scales 1/2, 1 and 2 -> (codes, scales, values)"""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    pieces = -(-k // 128)
+    v = torch.randint(-15, 16, (rows, pieces * 128), generator=g, device="cuda").float()
+    v[:, k:] = 0
+    scales = torch.randint(126, 129, (-(-rows // 128) if squares else rows, pieces), generator=g, device="cuda", dtype=torch.uint8)
+    unit = torch.exp2(scales.double() - 127)
+    if squares:
+        unit = unit.repeat_interleave(128, dim=0)[:rows]
+    return v.to(torch.float8_e4m3fn), scales, (v.double().view(rows, pieces, 128) * unit[:, :, None]).view(rows, -1)
+
+
+@pytest.mark.parametrize("rows,k,n", LARGE)
+@pytest.mark.parametrize("squares", [False, True])
+def test_tiles_are_exact(torch, rows, k, n, squares):
+    """Sums of whole numbers and quarters below 2^22 have no rounding: every tile shape equals the product in 64 bits."""
+    (xc, xs, x), (gc, gs, gate), (uc, us, up) = whole(torch, rows, k, False, 1), whole(torch, n, k, squares, 2), whole(torch, n, k, squares, 3)
+    g, v = x @ gate.t().contiguous(), x @ up.t().contiguous()
+    for kind in KINDS:
+        t = types(torch)[kind]
+        out, check = guarded(torch, (rows, n + 3), t)
+        B.patdnn_fp8_linear(xc, xs, gc, gs, None, out[:, :n])
+        check()
+        assert torch.equal(out[:, :n], g.float().to(t)) and bool((out[:, n:] == 77).all())
+        out, check = guarded(torch, (rows, n + 3), t)
+        B.patdnn_fp8_gated(xc, xs, gc, gs, uc, us, out[:, :n], act="relu")
+        check()
+        assert torch.equal(out[:, :n], (torch.relu(g).float() * v.float()).to(t)) and bool((out[:, n:] == 77).all())
+        out, check = guarded(torch, (rows, 2 * n + 3), t)
+        B.patdnn_fp8_gated_backward(torch.ones(rows, n, device="cuda", dtype=torch.bfloat16), xc, xs, gc, gs, uc, us, out[:, :2 * n], act="relu")
+        check()
+        want = torch.cat((torch.where(g > 0, v, 0.0), torch.relu(g)), dim=1).float().to(t)
+        assert torch.equal(out[:, :2 * n], want) and bool((out[:, 2 * n:] == 77).all())
+    h = torch.relu(g).float() * v.float()
+    pieces = -(-n // 128)
+    codes, check = guarded(torch, (rows, pieces * 128), torch.uint8)
+    scales, check2 = guarded(torch, (rows, pieces), torch.uint8)
+    B.patdnn_fp8_gated(xc, xs, gc, gs, uc, us, codes, scales=scales, act="relu", fp8=True)
+    check(), check2()
+    want = B.patdnn_fp8_quantize(h)
+    assert torch.equal(codes, want[0]) and torch.equal(scales, want[1])

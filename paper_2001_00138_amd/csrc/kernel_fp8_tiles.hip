@@ -42,12 +42,6 @@ __device__ __forceinline__ void wait_fetches()
 }
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-__device__ __forceinline__ intx4 buffer_of(const void* p)
-{
-    const uint64_t a = reinterpret_cast<uint64_t>(p);
-    return intx4{uniform((int)(uint32_t)a), uniform((int)(uint32_t)(a >> 32) & 0xffff), -1, 0x00020000};
-}
-
 // BN x BM rows of the weights and of x, on WN x WM wavefronts, NS stages in LDS.
 template <int BN, int BM, int WN, int WM, int NS>
 struct Tile {
@@ -55,8 +49,9 @@ struct Tile {
     static constexpr int kTN = BN / WN / 16, kTM = BM / WM / 16;         // matrix tiles of a wavefront
     static constexpr int kHN = kTN / 2, kHM = kTM > 1 ? kTM / 2 : 1;     // of a half
     static constexpr int kFetches = kRows / 8 / kWaves;                  // of 8 rows, per wavefront and stage
-    static constexpr int kStage = kRows * 128, kScales = NS * kStage, kLds = kScales + kRows * 4;
-    static_assert(kTN % 4 == 0 && (kTM == 1 || kTM % 2 == 0) && kRows % (8 * kWaves) == 0 && BN % 64 == 0 && BM % 16 == 0 && kRows <= kThreads, "shape");
+    static constexpr int kWords = (kRows + kThreads - 1) / kThreads;     // of scales, per thread
+    static constexpr int kStage = kRows * 128, kScales = NS * kStage, kLds = kScales + kWords * kThreads * 4;
+    static_assert(kTN % 4 == 0 && (kTM == 1 || kTM % 2 == 0) && kRows % (8 * kWaves) == 0 && BN % 64 == 0 && BM % 16 == 0, "shape");
     static_assert(NS == 2 || NS == 4, "stages by their place in a group of four");
 };
 
@@ -86,51 +81,69 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     auto side_of = [&](int row) { return row >= BN ? 2 : kTwo ? row >> 6 & 1 : 0; };
     auto row_of = [&](int row) { return row >= BN ? row - BN : kTwo ? (row >> 7) * 64 + (row & 63) : row; };
     const int w_last = A.s.out - 1 - n0, x_last = A.s.rows - 1 - m0;
-    const intx4 from_w = buffer_of(A.t.w + n0 * pitch), from_w2 = buffer_of(kTwo ? A.t.w2 + n0 * pitch : A.t.w), from_x = buffer_of(A.t.x + m0 * pitch);
+    const uint64_t bases[3] = {(uint64_t)(A.t.w + n0 * pitch), (uint64_t)((kTwo ? A.t.w2 : A.t.w) + n0 * pitch), (uint64_t)(A.t.x + m0 * pitch)};
+    auto buffer_of_side = [&](int side) {
+        const uint64_t p = side == 2 ? bases[2] : kTwo && side == 1 ? bases[1] : bases[0];
+        return intx4{uniform((int)(uint32_t)p), uniform((int)(uint32_t)(p >> 32) & 0xffff), -1, 0x00020000};
+    };
     const int fetch_row = wave * S::kFetches * 8;                        // this wavefront's first row
-    uint32_t data_at[S::kFetches];
-#pragma unroll
-    for (int i = 0; i < S::kFetches; ++i) {
-        const int first = fetch_row + i * 8, row = first + (lane >> 3);
-        const int swap = first < BN ? (row & 3) | (row >> 4 & 1) << 2 : row & 7;
-        data_at[i] = (uint32_t)(min(row_of(row), first < BN ? w_last : x_last) * (int)pitch) + (uint32_t)(((lane & 7) ^ swap) * 16);
-    }
+    const uint32_t w_end = (uint32_t)(w_last * (int)pitch), x_end = (uint32_t)(x_last * (int)pitch);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     auto fetch_stage = [&](int t) {
+        // (the lane's offsets are made again each time: eight registers of them would be spilled)
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        const uint32_t lane_at = (uint32_t)((l >> 3) * (int)pitch);
 #pragma unroll
         for (int i = 0; i < S::kFetches; ++i) {
             const int first = fetch_row + i * 8, side = side_of(first);
-            fetch16(side == 2 ? from_x : kTwo && side == 1 ? from_w2 : from_w, lds0 + (uint32_t)((t & (NS - 1)) * S::kStage + first * 128), data_at[i], (uint32_t)t * 128);
+            const uint32_t row = min(lane_at + (uint32_t)(row_of(first) * (int)pitch), side == 2 ? x_end : w_end);
+            const int swap = side == 2 ? l >> 3 : (l >> 3 & 3) | (first >> 4 & 1) << 2;
+            fetch16(buffer_of_side(side), lds0 + (uint32_t)uniform((t & (NS - 1)) * S::kStage + first * 128),
+                    row + (uint32_t)(((l & 7) ^ swap) * 16), (uint32_t)min(t, pieces - 1) * 128);
         }
     };
     // Scales of a group of four stages, a word for each row of LDS: in a register until the group before is done with LDS's.
-    const uint8_t* scales_at;
-    bool has_scales = (int)threadIdx.x < S::kRows;
-    {
-        const int row = (int)threadIdx.x, side = side_of(row);
+    const uint8_t* scales_at[S::kWords];
+#pragma unroll
+    for (int k = 0; k < S::kWords; ++k) {
+        const int row = min(k * S::kThreads + (int)threadIdx.x, S::kRows - 1), side = side_of(row);
         const uint8_t* from = side == 2 ? A.t.x_scales : kTwo && side == 1 ? A.t.w2_scales : A.t.w_scales;
         const int at = side == 2 ? m0 + min(row_of(row), x_last) : n0 + min(row_of(row), w_last);
-        scales_at = from + (long long)(side != 2 && A.s.squares ? at >> 7 : at) * pieces;
+        scales_at[k] = from + (long long)(side != 2 && A.s.squares ? at >> 7 : at) * pieces;
     }
-    uint32_t word = 0;
+    uint32_t words[S::kWords];
+    // (four bytes that lie in the row, the first of them stage t's after the shift)
     auto fetch_scales = [&](int t) {
-        if (!has_scales) return;
-        if (t + 4 <= pieces) {
-            word = __builtin_bit_cast(uint32_t, load_pack<uint8_t, 4>(scales_at + t));
-        } else {
-            word = 0;
-            for (int i = 0; i < pieces - t; ++i) word |= (uint32_t)scales_at[t + i] << (8 * i);
-        }
+        const int at = min(t, pieces - 4);
+#pragma unroll
+        for (int k = 0; k < S::kWords; ++k) words[k] = __builtin_bit_cast(uint32_t, load_pack<uint8_t, 4>(scales_at[k] + at)) >> (8 * min(t - at, 3));
     };
     auto put_scales = [&]() {
-        if (has_scales) *reinterpret_cast<uint32_t*>(lds + S::kScales + (int)threadIdx.x * 4) = word;
+#pragma unroll
+        for (int k = 0; k < S::kWords; ++k) *reinterpret_cast<uint32_t*>(lds + S::kScales + (k * S::kThreads + (int)threadIdx.x) * 4) = words[k];
     };
 
     const int wn = wave % WN, wm = wave / WN;
     const int a_row = wn * (16 * S::kTN) + (r >> 2) * 16 + (r & 3), b_row = BN + wm * (16 * S::kTM) + r;
-    const int a_at = a_row * 128 + (kb ^ ((r & 3) | (r >> 2 & 1) << 2)) * 16, b_at = b_row * 128 + (kb ^ (r & 7)) * 16;
-    auto chunks = [&](int at) {
-        return both_halves(*reinterpret_cast<const uint4*>(lds + at), *reinterpret_cast<const uint4*>(lds + (at ^ 64)));
+    // A lane's two chunks are kb and kb + 4, four chunks apart or four back.  (Four addresses that go from stage to stage: left to itself the compiler keeps one for
+    // each tile of each stage, which do not fit the registers.)
+    uint32_t from[4];
+    {
+        const uint32_t a_at = lds0 + (uint32_t)(a_row * 128 + (kb ^ ((r & 3) | (r >> 2 & 1) << 2)) * 16), b_at = lds0 + (uint32_t)(b_row * 128 + (kb ^ (r & 7)) * 16);
+        from[0] = a_at, from[1] = lds0 + ((a_at - lds0) ^ 64), from[2] = b_at, from[3] = lds0 + ((b_at - lds0) ^ 64);
+    }
+    auto go_on = [&](int by) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            from[i] += (uint32_t)by;
+            asm volatile("" : "+v"(from[i]));
+        }
+    };
+    auto chunks = [&](int first, int at) {
+        typedef const __attribute__((address_space(3))) intx4* lds_chunk;
+        const intx4 p = *(lds_chunk)(from[first] + (uint32_t)at), q = *(lds_chunk)(from[first + 1] + (uint32_t)at);
+        return int32x8{p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
     };
 
     floatx4 acc[S::kTN][S::kTM];
@@ -140,35 +153,45 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
         for (int j = 0; j < S::kTM; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     uint32_t sa[S::kTN], sb[S::kTM];
     int32x8 a[2][S::kHN], b[2][S::kHM];                  // halves; of a single tile of x: two stages
-    auto read_a = [&](int buffer, int half) {
+    auto read_a = [&](int half) {
 #pragma unroll
         for (int i = 0; i < S::kHN; ++i) {
             const int tile = half * S::kHN + i;
-            a[half][i] = chunks(buffer * S::kStage + a_at + ((tile >> 2) * 64 + (tile & 3) * 4) * 128);
+            a[half][i] = chunks(0, ((tile >> 2) * 64 + (tile & 3) * 4) * 128);
         }
     };
-    auto read_b = [&](int buffer, int half) {
+    auto read_b = [&](int half) {
 #pragma unroll
-        for (int j = 0; j < S::kHM; ++j) b[half][j] = chunks(buffer * S::kStage + b_at + (S::kTM > 1 ? half * S::kHM + j : 0) * 16 * 128);
+        for (int j = 0; j < S::kHM; ++j) b[half][j] = chunks(2, (S::kTM > 1 ? half * S::kHM + j : 0) * 16 * 128);
     };
 
-    fetch_scales(0);
-    for (int t = 0; t < min(NS, pieces); ++t) fetch_stage(t);
+    if (pieces >= 4) {
+        fetch_scales(0);
+    } else {
+#pragma unroll
+        for (int k = 0; k < S::kWords; ++k) {
+            words[k] = 0;
+            for (int i = 0; i < pieces; ++i) words[k] |= (uint32_t)scales_at[k][i] << (8 * i);
+        }
+    }
+    for (int t = 0; t < NS; ++t) fetch_stage(t);
     put_scales();
     wait_fetches<0>();
     meet();
-    read_a(0, 0);
-    read_b(0, 0);
+    read_a(0);
+    read_b(0);
 
-    auto stage = [&](auto step, int t) {
-        constexpr int STEP = decltype(step)::value, F = STEP & 1, HERE = STEP & (NS - 1), NEXT = (STEP + 1) & (NS - 1);
+    // Stage t, at place STEP of its group of four; LOOP: a whole group.  No branches: around them the compiler would move products, and hold their operands
+    // longer.  Behind the last stage it is fetched again, and what LDS holds is read and not used.
+    auto stage = [&](auto step, auto loop, int t) {
+        constexpr int STEP = decltype(step)::value, LOOP = decltype(loop)::value, F = STEP & 1, HERE = STEP & (NS - 1), NEXT = (STEP + 1) & (NS - 1);
         if (STEP == 0) {
 #pragma unroll
             for (int i = 0; i < S::kTN; ++i)
                 sa[i] = *reinterpret_cast<const uint32_t*>(lds + S::kScales + (a_row + (i >> 2) * 64 + (i & 3) * 4) * 4);
 #pragma unroll
             for (int j = 0; j < S::kTM; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(lds + S::kScales + (b_row + j * 16) * 4);
-            if (t + 4 < pieces) fetch_scales(t + 4);
+            if (LOOP) fetch_scales(t + 4);
         }
         auto multiply = [&](int ha, int hb) {
 #pragma unroll
@@ -197,41 +220,50 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
                 for (int m = 0; m < S::kTM; ++m) acc[n][m] = multiply_wide(w, wide[EXACT ? m : 0], acc[n][m]);
             }
         };
-        if (S::kTM > 1) read_b(HERE, F ^ 1);
+        // (the compiler would read earlier than that, and spill)
+        auto phase = [] { __builtin_amdgcn_sched_barrier(0); };
+        if (S::kTM > 1) read_b(F ^ 1);
         if constexpr (EXACT) {
-            read_a(HERE, 1);
+            read_a(1);
             widen_b(F);
             if (S::kTM > 1) widen_b(F ^ 1);
             multiply_half(0);
         } else {
             multiply(0, F);
-            read_a(HERE, 1);
+            phase();
+            read_a(1);
             if (S::kTM > 1) multiply(0, F ^ 1);
+            phase();
         }
-        if (t + 1 < pieces) {
-            // the next stage has arrived once no more than those behind it are on their way
-            if (NS > 2 && t + NS <= pieces) wait_fetches<(NS - 2) * S::kFetches>();
-            else wait_fetches<0>();
-            if (STEP == 3) put_scales();
-            meet();
-            if (t + NS < pieces) fetch_stage(t + NS);
-            read_a(NEXT, 0);
-        }
+        // the next stage has arrived once no more than those behind it are on their way
+        wait_fetches<(NS - 2) * S::kFetches>();
+        if (STEP == 3) put_scales();
+        meet();
+        fetch_stage(t + NS);
+        go_on((NEXT - HERE) * S::kStage);
+        read_a(0);
         if constexpr (EXACT) {
             multiply_half(1);
-            if (t + 1 < pieces) read_b(NEXT, F ^ 1);
+            read_b(F ^ 1);
         } else {
             if (S::kTM > 1) multiply(1, F ^ 1);
-            if (t + 1 < pieces) read_b(NEXT, F ^ 1);
+            phase();
+            read_b(F ^ 1);
             multiply(1, F);
+            phase();
         }
     };
-    for (int t = 0; t < pieces; t += 4) {
-        stage(Const<0>{}, t);
-        if (t + 1 < pieces) stage(Const<1>{}, t + 1);
-        if (t + 2 < pieces) stage(Const<2>{}, t + 2);
-        if (t + 3 < pieces) stage(Const<3>{}, t + 3);
+    int t = 0;
+    for (; t + 4 <= pieces; t += 4) {
+        stage(Const<0>{}, Const<1>{}, t);
+        stage(Const<1>{}, Const<1>{}, t + 1);
+        stage(Const<2>{}, Const<1>{}, t + 2);
+        stage(Const<3>{}, Const<1>{}, t + 3);
     }
+    if (t < pieces) stage(Const<0>{}, Const<0>{}, t);
+    if (t + 1 < pieces) stage(Const<1>{}, Const<0>{}, t + 1);
+    if (t + 2 < pieces) stage(Const<2>{}, Const<0>{}, t + 2);
+    wait_fetches<0>();
 
     // A lane's results: row m0 + ... + r of x, sixteen neighbouring outputs for each four tiles (and their other sums four tiles on).
     constexpr int kGroups = kTwo ? 1 : S::kTN / 4;

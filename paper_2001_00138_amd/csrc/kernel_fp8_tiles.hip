@@ -42,15 +42,44 @@ __device__ __forceinline__ void wait_fetches()
 }
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// fp8_multiply with the sums kept where they are, in the accumulation registers: the compiler would give them new ones with every product, and move them back in
+// every round, for which there is no room.  What it does not see here it need not see: the operands were waited for before; a result is read by another
+// product no sooner than three behind it, and by other instructions only after let_settle().  (The wait is for scales that a vector instruction has just moved.)
+template <int BYTE_A, int BYTE_B>
+__device__ __forceinline__ void multiply_in_place(const int32x8& a, const int32x8& b, floatx4& c, uint32_t sa, uint32_t sb)
+{
+    asm("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
+        : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb), "n"(BYTE_A & 1), "n"(BYTE_B & 1), "n"(BYTE_A >> 1), "n"(BYTE_B >> 1));
+}
+// (the bytes' places are constants once the loops around are unrolled)
+__device__ __forceinline__ void multiply_tile(const int32x8& a, const int32x8& b, floatx4& c, uint32_t sa, uint32_t sb, int byte_a, int byte_b)
+{
+    auto with_b = [&](auto i, auto j) { multiply_in_place<decltype(i)::value, decltype(j)::value>(a, b, c, sa, sb); };
+    auto with_a = [&](auto i) { byte_b == 0 ? with_b(i, Const<0>{}) : byte_b == 1 ? with_b(i, Const<1>{}) : byte_b == 2 ? with_b(i, Const<2>{}) : with_b(i, Const<3>{}); };
+    byte_a == 0 ? with_a(Const<0>{}) : byte_a == 1 ? with_a(Const<1>{}) : byte_a == 2 ? with_a(Const<2>{}) : with_a(Const<3>{});
+}
+// The last products' results may be read 18 wait states after them.
+template <int N, int M>
+__device__ __forceinline__ void let_settle(floatx4 (&acc)[N][M])
+{
+    asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < M; ++j) asm volatile("" : "+a"(acc[i][j]));
+}
+
 // BN x BM rows of the weights and of x, on WN x WM wavefronts, NS stages in LDS.
 template <int BN, int BM, int WN, int WM, int NS>
 struct Tile {
     static constexpr int kWaves = WN * WM, kThreads = 64 * kWaves, kRows = BN + BM;
     static constexpr int kTN = BN / WN / 16, kTM = BM / WM / 16;         // matrix tiles of a wavefront
-    static constexpr int kHN = kTN / 2, kHM = kTM > 1 ? kTM / 2 : 1;     // of a half
+    static constexpr int kHN = kTN / 2, kHM = kTM > 1 ? kTM / 2 : 1, kPart = kHN / 2;    // of a half, of a part of one
     static constexpr int kFetches = kRows / 8 / kWaves;                  // of 8 rows, per wavefront and stage
     static constexpr int kWords = (kRows + kThreads - 1) / kThreads;     // of scales, per thread
-    static constexpr int kStage = kRows * 128, kScales = NS * kStage, kLds = kScales + kWords * kThreads * 4;
+    // Scales of a stage: a word for a lane's four neighbouring tiles of the weights, one for as many of x.
+    static constexpr int kGroupsN = kTN / 4, kGroupsM = (kTM + 3) / 4, kScaleStage = BN + WM * kGroupsM * 64;
+    static constexpr int kStage = kRows * 128, kScales = NS * kStage, kLds = kScales + 8 * kScaleStage;
     static_assert(kTN % 4 == 0 && (kTM == 1 || kTM % 2 == 0) && kRows % (8 * kWaves) == 0 && BN % 64 == 0 && BM % 16 == 0, "shape");
     static_assert(NS == 2 || NS == 4, "stages by their place in a group of four");
 };
@@ -81,14 +110,20 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     auto side_of = [&](int row) { return row >= BN ? 2 : kTwo ? row >> 6 & 1 : 0; };
     auto row_of = [&](int row) { return row >= BN ? row - BN : kTwo ? (row >> 7) * 64 + (row & 63) : row; };
     const int w_last = A.s.out - 1 - n0, x_last = A.s.rows - 1 - m0;
-    const uint64_t bases[3] = {(uint64_t)(A.t.w + n0 * pitch), (uint64_t)((kTwo ? A.t.w2 : A.t.w) + n0 * pitch), (uint64_t)(A.t.x + m0 * pitch)};
-    auto buffer_of_side = [&](int side) {
-        const uint64_t p = side == 2 ? bases[2] : kTwo && side == 1 ? bases[1] : bases[0];
-        return intx4{uniform((int)(uint32_t)p), uniform((int)(uint32_t)(p >> 32) & 0xffff), -1, 0x00020000};
-    };
     const int fetch_row = wave * S::kFetches * 8;                        // this wavefront's first row
     const uint32_t w_end = (uint32_t)(w_last * (int)pitch), x_end = (uint32_t)(x_last * (int)pitch);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    // of each fetch, in scalar registers: where its side's rows begin, how far behind that its eight and the side's last one are
+    int low[S::kFetches], high[S::kFetches], row_at[S::kFetches], end_at[S::kFetches];
+#pragma unroll
+    for (int i = 0; i < S::kFetches; ++i) {
+        const int first = fetch_row + i * 8, side = side_of(first);
+        const uint8_t* p = side == 2 ? A.t.x + m0 * pitch : (kTwo && side == 1 ? A.t.w2 : A.t.w) + n0 * pitch;
+        low[i] = uniform((int)(uint32_t)(uint64_t)p);
+        high[i] = uniform((int)((uint64_t)p >> 32 & 0xffff));
+        row_at[i] = uniform(row_of(first) * (int)pitch);
+        end_at[i] = uniform((int)(side == 2 ? x_end : w_end));
+    }
     auto fetch_stage = [&](int t) {
         // (the lane's offsets are made again each time: eight registers of them would be spilled)
         int l = lane;
@@ -96,14 +131,15 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
         const uint32_t lane_at = (uint32_t)((l >> 3) * (int)pitch);
 #pragma unroll
         for (int i = 0; i < S::kFetches; ++i) {
-            const int first = fetch_row + i * 8, side = side_of(first);
-            const uint32_t row = min(lane_at + (uint32_t)(row_of(first) * (int)pitch), side == 2 ? x_end : w_end);
-            const int swap = side == 2 ? l >> 3 : (l >> 3 & 3) | (first >> 4 & 1) << 2;
-            fetch16(buffer_of_side(side), lds0 + (uint32_t)uniform((t & (NS - 1)) * S::kStage + first * 128),
-                    row + (uint32_t)(((l & 7) ^ swap) * 16), (uint32_t)min(t, pieces - 1) * 128);
+            const int first = fetch_row + i * 8;
+            const uint32_t row = min(lane_at + (uint32_t)row_at[i], (uint32_t)end_at[i]);
+            const int mask = first < BN ? 3 : 7, more = first < BN ? (first >> 4 & 1) << 2 : 0;
+            fetch16(intx4{low[i], high[i], -1, 0x00020000}, lds0 + (uint32_t)uniform((t & (NS - 1)) * S::kStage + first * 128),
+                    row + (uint32_t)(((l & 7) ^ ((l >> 3 & mask) | more)) * 16), (uint32_t)min(t, pieces - 1) * 128);
         }
     };
-    // Scales of a group of four stages, a word for each row of LDS: in a register until the group before is done with LDS's.
+    // Scales of a group of four stages, four bytes for each row of LDS: in a register for three stages, then in LDS, where two groups have a place.
+    // There a word is what a lane needs for four tiles: the matrix instruction selects its byte.
     const uint8_t* scales_at[S::kWords];
 #pragma unroll
     for (int k = 0; k < S::kWords; ++k) {
@@ -113,15 +149,21 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
         scales_at[k] = from + (long long)(side != 2 && A.s.squares ? at >> 7 : at) * pieces;
     }
     uint32_t words[S::kWords];
-    // (four bytes that lie in the row, the first of them stage t's after the shift)
+    // (four bytes that lie in the row: in its last group those before it come along, and are shifted out)
     auto fetch_scales = [&](int t) {
         const int at = min(t, pieces - 4);
 #pragma unroll
-        for (int k = 0; k < S::kWords; ++k) words[k] = __builtin_bit_cast(uint32_t, load_pack<uint8_t, 4>(scales_at[k] + at)) >> (8 * min(t - at, 3));
+        for (int k = 0; k < S::kWords; ++k) words[k] = __builtin_bit_cast(uint32_t, load_pack<uint8_t, 4>(scales_at[k] + at));
     };
-    auto put_scales = [&]() {
+    auto put_scales = [&](int group, int shift) {
 #pragma unroll
-        for (int k = 0; k < S::kWords; ++k) *reinterpret_cast<uint32_t*>(lds + S::kScales + (k * S::kThreads + (int)threadIdx.x) * 4) = words[k];
+        for (int k = 0; k < S::kWords; ++k) {
+            const int row = min(k * S::kThreads + (int)threadIdx.x, S::kRows - 1), m = row - BN;
+            const int at = row < BN ? (row & ~63) + ((row >> 4 & 3) * 4 + (row & 3)) * 4 + (row >> 2 & 3)
+                                    : BN + (m / (16 * S::kTM) * S::kGroupsM + (m / 16 % S::kTM) / 4) * 64 + (m & 15) * 4 + (m / 16 % S::kTM) % 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lds[S::kScales + ((group & 1) * 4 + i) * S::kScaleStage + at] = (char)(words[k] >> shift >> (8 * i));
+        }
     };
 
     const int wn = wave % WN, wm = wave / WN;
@@ -151,14 +193,22 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     for (int i = 0; i < S::kTN; ++i)
 #pragma unroll
         for (int j = 0; j < S::kTM; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    uint32_t sa[S::kTN], sb[S::kTM];
+    uint32_t sa[S::kGroupsN], sb[S::kGroupsM], next_sa[S::kGroupsN], next_sb[S::kGroupsM];
     int32x8 a[2][S::kHN], b[2][S::kHM];                  // halves; of a single tile of x: two stages
-    auto read_a = [&](int half) {
+    // (part: two of a half's four tiles)
+    auto read_a = [&](int half, int part) {
 #pragma unroll
-        for (int i = 0; i < S::kHN; ++i) {
+        for (int i = part * S::kPart; i < (part + 1) * S::kPart; ++i) {
             const int tile = half * S::kHN + i;
             a[half][i] = chunks(0, ((tile >> 2) * 64 + (tile & 3) * 4) * 128);
         }
+    };
+    auto read_scales = [&](int t) {
+        const char* at = lds + S::kScales + (t & 7) * S::kScaleStage + r * 4;
+#pragma unroll
+        for (int g = 0; g < S::kGroupsN; ++g) next_sa[g] = *reinterpret_cast<const uint32_t*>(at + wn * (16 * S::kTN) + g * 64);
+#pragma unroll
+        for (int g = 0; g < S::kGroupsM; ++g) next_sb[g] = *reinterpret_cast<const uint32_t*>(at + BN + (wm * S::kGroupsM + g) * 64);
     };
     auto read_b = [&](int half) {
 #pragma unroll
@@ -175,31 +225,30 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
         }
     }
     for (int t = 0; t < NS; ++t) fetch_stage(t);
-    put_scales();
+    put_scales(0, 0);
     wait_fetches<0>();
     meet();
-    read_a(0);
+    read_scales(0);
+    read_a(0, 0);
+    read_a(0, 1);
     read_b(0);
 
     // Stage t, at place STEP of its group of four; LOOP: a whole group.  No branches: around them the compiler would move products, and hold their operands
     // longer.  Behind the last stage it is fetched again, and what LDS holds is read and not used.
     auto stage = [&](auto step, auto loop, int t) {
         constexpr int STEP = decltype(step)::value, LOOP = decltype(loop)::value, F = STEP & 1, HERE = STEP & (NS - 1), NEXT = (STEP + 1) & (NS - 1);
-        if (STEP == 0) {
 #pragma unroll
-            for (int i = 0; i < S::kTN; ++i)
-                sa[i] = *reinterpret_cast<const uint32_t*>(lds + S::kScales + (a_row + (i >> 2) * 64 + (i & 3) * 4) * 4);
+        for (int g = 0; g < S::kGroupsN; ++g) sa[g] = next_sa[g];
 #pragma unroll
-            for (int j = 0; j < S::kTM; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(lds + S::kScales + (b_row + j * 16) * 4);
-            if (LOOP) fetch_scales(t + 4);
-        }
-        auto multiply = [&](int ha, int hb) {
+        for (int g = 0; g < S::kGroupsM; ++g) sb[g] = next_sb[g];
+        if (STEP == 0 && LOOP) fetch_scales(t + 4);
+        auto multiply = [&](int ha, int part, int hb) {
 #pragma unroll
-            for (int i = 0; i < S::kHN; ++i)
+            for (int i = part * S::kPart; i < (part + 1) * S::kPart; ++i)
 #pragma unroll
                 for (int j = 0; j < S::kHM; ++j) {
                     const int n = ha * S::kHN + i, m = (S::kTM > 1 ? hb * S::kHM : 0) + j;
-                    acc[n][m] = fp8_multiply<STEP>(a[ha][i], b[hb][j], acc[n][m], sa[n], sb[m]);
+                    multiply_tile(a[ha][i], b[hb][j], acc[n][m], sa[n / 4], sb[m / 4], n % 4, m % 4);
                 }
         };
         // (in bfloat16 a tile of x is made once a stage, one of the weights where it is multiplied with all of x's)
@@ -208,48 +257,63 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
 #pragma unroll
             for (int j = 0; j < S::kHM; ++j) {
                 const int m = (S::kTM > 1 ? hb * S::kHM : 0) + j;
-                wide[EXACT ? m : 0] = fp8_widen(b[hb][j], (sb[m] >> (8 * STEP) & 255) << 23);
+                wide[EXACT ? m : 0] = fp8_widen(b[hb][j], (sb[m / 4] >> (8 * (m % 4)) & 255) << 23);
             }
         };
         auto multiply_half = [&](int ha) {
 #pragma unroll
             for (int i = 0; i < S::kHN; ++i) {
                 const int n = ha * S::kHN + i;
-                const Wide w = fp8_widen(a[ha][i], (sa[n] >> (8 * STEP) & 255) << 23);
+                const Wide w = fp8_widen(a[ha][i], (sa[n / 4] >> (8 * (n % 4)) & 255) << 23);
 #pragma unroll
                 for (int m = 0; m < S::kTM; ++m) acc[n][m] = multiply_wide(w, wide[EXACT ? m : 0], acc[n][m]);
             }
         };
-        // (the compiler would read earlier than that, and spill)
+        // What is read takes the place of what has been multiplied.  (The compiler would read earlier, and spill.)
         auto phase = [] { __builtin_amdgcn_sched_barrier(0); };
+        auto next_stage = [&] {
+            // it has arrived once no more than those behind it are on their way
+            wait_fetches<(NS - 2) * S::kFetches>();
+            if (STEP == 3) put_scales((t >> 2) + 1, 8 * max(0, min(t + 5 - pieces, 3)));
+            meet();
+            fetch_stage(t + NS);
+            go_on((NEXT - HERE) * S::kStage);
+            read_scales(t + 1);
+        };
         if (S::kTM > 1) read_b(F ^ 1);
         if constexpr (EXACT) {
-            read_a(1);
+            read_a(1, 0);
+            read_a(1, 1);
             widen_b(F);
             if (S::kTM > 1) widen_b(F ^ 1);
             multiply_half(0);
-        } else {
-            multiply(0, F);
-            phase();
-            read_a(1);
-            if (S::kTM > 1) multiply(0, F ^ 1);
-            phase();
-        }
-        // the next stage has arrived once no more than those behind it are on their way
-        wait_fetches<(NS - 2) * S::kFetches>();
-        if (STEP == 3) put_scales();
-        meet();
-        fetch_stage(t + NS);
-        go_on((NEXT - HERE) * S::kStage);
-        read_a(0);
-        if constexpr (EXACT) {
+            next_stage();
+            read_a(0, 0);
+            read_a(0, 1);
             multiply_half(1);
             read_b(F ^ 1);
         } else {
-            if (S::kTM > 1) multiply(1, F ^ 1);
+            multiply(0, 0, F);
+            multiply(0, 1, F);
+            phase();
+            if (S::kTM > 1) multiply(0, 0, F ^ 1);
+            phase();
+            read_a(1, 0);
+            read_a(1, 1);
+            if (S::kTM > 1) multiply(0, 1, F ^ 1);
+            phase();
+            next_stage();
+            if (S::kTM > 1) {
+                multiply(1, 0, F ^ 1);
+                multiply(1, 1, F ^ 1);
+            }
             phase();
             read_b(F ^ 1);
-            multiply(1, F);
+            read_a(0, 0);
+            multiply(1, 0, F);
+            phase();
+            read_a(0, 1);
+            multiply(1, 1, F);
             phase();
         }
     };
@@ -264,6 +328,8 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     if (t + 1 < pieces) stage(Const<1>{}, Const<0>{}, t + 1);
     if (t + 2 < pieces) stage(Const<2>{}, Const<0>{}, t + 2);
     wait_fetches<0>();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!EXACT) let_settle(acc);
 
     // A lane's results: row m0 + ... + r of x, sixteen neighbouring outputs for each four tiles (and their other sums four tiles on).
     constexpr int kGroups = kTwo ? 1 : S::kTN / 4;
@@ -365,7 +431,7 @@ hipError_t launch_shape(Args A, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Rows of x a tile: the largest that give every CU one.
+// Tiles of bn outputs x bm rows.
 long long tiles_of(const ProductShape& s, int bn, int bm) { return ceil_div(s.out, bn) * ceil_div(s.rows, bm); }
 
 }  // namespace

@@ -781,24 +781,29 @@ def patdnn_group_norm_workspace_floats(n: int, pixels: int, channels: int, group
 # the feed-forward block in fp8: norm of rows, codes, linear layer, gated projections
 # ---------------------------------------------------------------------------
 
-def _call(like, stream, f, *args) -> None:
-    """f(*args, stream) with like's device current: without a stream its current one."""
-    torch = _torch()
-    index = like.device.index
-    if index == torch._C._cuda_getDevice():
-        _check(f(*args, _stream_ptr(stream)))
+def _call(device: int, stream, f, *args) -> None:
+    """f(*args, stream) with this device current: without a stream its current one."""
+    torch = _modules["torch"]
+    if device == torch._C._cuda_getDevice():
+        status = f(*args, (torch._C._cuda_getCurrentRawStream(device) or None) if stream is None else _stream_ptr(stream))
     else:
-        with torch.cuda.device(index):
-            _check(f(*args, _stream_ptr(stream)))
+        with torch.cuda.device(device):
+            status = f(*args, _stream_ptr(stream))
+    if status:
+        _check(status)
 
 
-def _together(like, *tensors) -> None:
+def _together(like, *tensors) -> int:
+    """The device of all these tensors."""
+    if not _modules:
+        _torch()
     if not like.is_cuda:
         raise ValueError("device tensor expected")
-    device = like.device
+    device = like.get_device()
     for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"all tensors must be on one device: {t.device} and {device}")
+        if t is not None and (not t.is_cuda or t.get_device() != device):
+            raise ValueError(f"all tensors must be on one device: {t.device} and {like.device}")
+    return device
 
 
 def _typed_rows(t, shape, dtype, name: str) -> int:
@@ -810,25 +815,42 @@ def _typed_rows(t, shape, dtype, name: str) -> int:
 
 def _byte_codes(t, name: str):
     """Codes, as bytes or as torch's type of them."""
-    torch = _torch()
+    torch = _modules["torch"]
     if t.dtype != torch.uint8 and t.dtype != torch.float8_e4m3fn:
         raise ValueError(f"{name} must be uint8 or float8_e4m3fn")
-    if t.dim() != 2 or t.shape[1] == 0 or t.shape[1] % 128:
+    shape = t.shape
+    if len(shape) != 2 or shape[1] == 0 or shape[1] % 128:
         raise ValueError(f"{name} must be [rows, whole pieces of 128]")
     return _devptr(t)
 
 
 def _byte_scales(t, rows: int, pieces: int, name: str, blocks=None):
     """Scales of codes [rows, pieces * 128] -> (their pointer, how they are laid out; of one row both layouts are the same)."""
-    torch = _torch()
+    torch = _modules["torch"]
     if t.dtype != torch.uint8 and t.dtype != torch.float8_e8m0fnu:
         raise ValueError(f"{name} must be uint8 or float8_e8m0fnu")
-    shape = tuple(t.shape)
-    if shape == (rows, pieces) and blocks != 1:
-        return _devptr(t), 0
-    if shape == (-(-rows // 128), pieces) and blocks != 0:
-        return _devptr(t), 1
+    shape = t.shape
+    if len(shape) == 2 and shape[1] == pieces:
+        if shape[0] == rows and blocks != 1:
+            return _devptr(t), 0
+        if shape[0] == -(-rows // 128) and blocks != 0:
+            return _devptr(t), 1
     raise ValueError(f"{name} must be {(rows, pieces)}" + ("" if blocks == 0 else f" or {(-(-rows // 128), pieces)}"))
+
+
+def _new_codes(out, scales, rows: int, pieces: int, like, stream, name="output"):
+    """Codes with blocks along the rows, and their scales, as given or allocated -> (codes, scales, their pointers)."""
+    if out is None:
+        out = _new((rows, pieces * 128), _modules["torch"].uint8, like, stream)
+        op = out.data_ptr()
+    else:
+        if tuple(out.shape) != (rows, pieces * 128):
+            raise ValueError(f"{name} must be {(rows, pieces * 128)}")
+        op = _byte_codes(out, name)
+    if scales is None:
+        scales = _new((rows, pieces), _modules["torch"].uint8, like, stream)
+        return out, scales, op, scales.data_ptr()
+    return out, scales, op, _byte_scales(scales, rows, pieces, "scales", 0)[0]
 
 
 def patdnn_fp8_quantize(x, codes=None, scales=None, *, blocks="rows", transposed=False, stream=None):
@@ -839,43 +861,49 @@ def patdnn_fp8_quantize(x, codes=None, scales=None, *, blocks="rows", transposed
         kind = FP8_BLOCKS[blocks]
     except KeyError:
         raise ValueError(f"blocks must be one of {', '.join(FP8_BLOCKS)}") from None
-    _together(x, codes, scales)
+    device = _together(x, codes, scales)
     row = _rows(x, "x")
     rows, cols = x.shape
     r, c = (cols, rows) if transposed else (rows, cols)
     pieces = -(-c // 128)
-    if codes is None:
-        codes = _new((r, pieces * 128), torch.uint8, x, stream)
-    elif tuple(codes.shape) != (r, pieces * 128):
-        raise ValueError(f"codes must be {(r, pieces * 128)}")
-    if scales is None:
-        scales = _new((-(-r // 128) if kind else r, pieces), torch.uint8, x, stream)
-    cp = _byte_codes(codes, "codes") if codes.numel() else _devptr(codes)
-    sp, _ = _byte_scales(scales, r, pieces, "scales", kind if r != 1 else None)
-    _call(x, stream, lib().patdnn_fp8_quantize, x.data_ptr(), _type(x.dtype), rows, cols, row, kind, int(bool(transposed)), cp, sp)
+    if not kind:
+        codes, scales, cp, sp = _new_codes(codes, scales, r, pieces, x, stream, "codes")
+    else:
+        if codes is None:
+            codes = _new((r, pieces * 128), torch.uint8, x, stream)
+        elif tuple(codes.shape) != (r, pieces * 128):
+            raise ValueError(f"codes must be {(r, pieces * 128)}")
+        if scales is None:
+            scales = _new((-(-r // 128), pieces), torch.uint8, x, stream)
+        cp = _byte_codes(codes, "codes") if codes.numel() else _devptr(codes)
+        sp, _ = _byte_scales(scales, r, pieces, "scales", kind if r != 1 else None)
+    _call(device, stream, lib().patdnn_fp8_quantize, x.data_ptr(), _type(x.dtype), rows, cols, row, kind, 1 if transposed else 0, cp, sp)
     return codes, scales
 
 
 def patdnn_fp8_dequantize(codes, scales, cols: int, out=None, *, dtype=None, stream=None):
     """The values [rows, cols] that codes and scales (of either layout) stand for, float32 unless ``out`` or ``dtype`` says otherwise."""
     torch = _torch()
-    _together(codes, scales, out)
+    device = _together(codes, scales, out)
     cp = _byte_codes(codes, "codes")
     rows, pieces = codes.shape[0], codes.shape[1] // 128
     if not 0 < cols <= pieces * 128 or cols <= (pieces - 1) * 128:
         raise ValueError(f"{cols} columns are not {pieces} pieces of 128")
     sp, kind = _byte_scales(scales, rows, pieces, "scales")
     if out is None:
-        out = _new((rows, cols), dtype or torch.float32, codes, stream)
-    elif tuple(out.shape) != (rows, cols) or (dtype and out.dtype != dtype):
-        raise ValueError(f"output must be {(rows, cols)}, of type dtype if that is given")
-    _call(codes, stream, lib().patdnn_fp8_dequantize, cp, sp, rows, cols, kind, out.data_ptr(), _type(out.dtype), _rows(out, "output"))
+        out, row = _new((rows, cols), dtype or torch.float32, codes, stream), cols
+    else:
+        if tuple(out.shape) != (rows, cols) or (dtype and out.dtype != dtype):
+            raise ValueError(f"output must be {(rows, cols)}, of type dtype if that is given")
+        row = _rows(out, "output")
+    _call(device, stream, lib().patdnn_fp8_dequantize, cp, sp, rows, cols, kind, out.data_ptr(), _type(out.dtype), row)
     return out
 
 
 def _row_floats(t, count: int, name: str, like, stream):
     if t is None:
-        t = _new((count,), _torch().float32, like, stream)
+        t = _new((count,), _modules["torch"].float32, like, stream)
+        return t, t.data_ptr()
     return t, _float_vector(t, count, name)
 
 
@@ -884,50 +912,42 @@ def patdnn_rms_norm(x, gamma=None, out=None, *, residual=None, sum=None, eps=1e-
 
     gamma: float32 [cols] or None.  out: x's type, ``dtype``'s, or (``fp8``) the codes of patdnn_fp8_quantize, with their scales (None otherwise).
     sum: x + residual in x's type, x itself without a residual; ``sum=residual`` adds in place.  rstd: float32 [rows], for the backward call."""
-    torch = _torch()
-    _together(x, gamma, out, residual, sum, scales, rstd)
+    device = _together(x, gamma, out, residual, sum, scales, rstd)
     x_row = _rows(x, "x")
-    rows, cols = x.shape
-    kind = _type(x.dtype)
+    shape, x_type = x.shape, x.dtype
+    rows, cols = shape
     residual_row = sum_row = 0
+    rp = total = None
     if residual is not None:
-        residual_row = _typed_rows(residual, x.shape, x.dtype, "residual")
+        residual_row, rp = _typed_rows(residual, shape, x_type, "residual"), residual.data_ptr()
         if sum is None:
-            sum = _new((rows, cols), x.dtype, x, stream)
+            sum = _new((rows, cols), x_type, x, stream)
     if sum is not None:
-        sum_row = _typed_rows(sum, x.shape, x.dtype, "sum")
+        sum_row, total = _typed_rows(sum, shape, x_type, "sum"), sum.data_ptr()
     if fp8:
-        pieces = -(-cols // 128)
         if dtype is not None:
             raise ValueError("dtype is for results that are no codes")
-        if out is None:
-            out = _new((rows, pieces * 128), torch.uint8, x, stream)
-        elif tuple(out.shape) != (rows, pieces * 128):
-            raise ValueError(f"output must be {(rows, pieces * 128)}")
-        if scales is None:
-            scales = _new((rows, pieces), torch.uint8, x, stream)
-        y_type, y_row, yp = PATDNN_FP8, 0, _byte_codes(out, "output")
-        sp, _ = _byte_scales(scales, rows, pieces, "scales", 0)
+        out, scales, yp, sp = _new_codes(out, scales, rows, -(-cols // 128), x, stream)
+        y_type, y_row = PATDNN_FP8, 0
     else:
         if scales is not None:
             raise ValueError("scales are for codes")
         if out is None:
-            out = _new((rows, cols), dtype or x.dtype, x, stream)
-        elif out.shape != x.shape or (dtype and out.dtype != dtype):
+            out = _new((rows, cols), dtype or x_type, x, stream)
+        elif out.shape != shape or (dtype and out.dtype != dtype):
             raise ValueError("output must have the shape of x, and type dtype if that is given")
         y_type, y_row, yp, sp = _type(out.dtype), _rows(out, "output"), out.data_ptr(), None
-    rstd, rp = _row_floats(rstd, rows, "rstd", x, stream)
-    desc = RmsDesc(rows, cols, kind, y_type, eps, x_row, residual_row, sum_row, y_row)
-    _call(x, stream, lib().patdnn_rms_norm, ctypes.byref(desc), x.data_ptr(), None if residual is None else residual.data_ptr(),
-          _float_vector(gamma, cols, "gamma"), None if sum is None else sum.data_ptr(), yp, sp, rp)
+    rstd, root = _row_floats(rstd, rows, "rstd", x, stream)
+    desc = RmsDesc(rows, cols, _type(x_type), y_type, eps, x_row, residual_row, sum_row, y_row)
+    _call(device, stream, lib().patdnn_rms_norm, ctypes.byref(desc), x.data_ptr(), rp, _float_vector(gamma, cols, "gamma"), total, yp, sp, root)
     return out, scales, x if sum is None else sum, rstd
 
 
 def patdnn_rms_norm_backward(dy, sum, rstd, gamma=None, out=None, *, dsum=None, dgamma=None, workspace=None, stream=None):
     """Gradients of patdnn_rms_norm: (dx like sum, dgamma float32 [cols]) from dy (of any type), the forward call's sum and rstd.  ``dsum``: the gradient that
     arrives along the residual stream, added to dx; ``out=dsum`` adds in place."""
-    torch = _torch()
-    _together(sum, dy, rstd, gamma, out, dsum, dgamma, workspace)
+    device = _together(sum, dy, rstd, gamma, out, dsum, dgamma, workspace)
+    torch = _modules["torch"]
     s_row = _rows(sum, "sum")
     rows, cols = sum.shape
     if dy.shape != sum.shape:
@@ -941,7 +961,7 @@ def patdnn_rms_norm_backward(dy, sum, rstd, gamma=None, out=None, *, dsum=None, 
         workspace = _new((lib().patdnn_rms_norm_workspace_floats(ctypes.byref(desc)),), torch.float32, sum, stream)
     elif workspace.dtype != torch.float32:
         raise ValueError("workspace must be a float32 tensor")
-    _call(sum, stream, lib().patdnn_rms_norm_backward, ctypes.byref(desc), dy.data_ptr(), None if dsum is None else dsum.data_ptr(), sum.data_ptr(),
+    _call(device, stream, lib().patdnn_rms_norm_backward, ctypes.byref(desc), dy.data_ptr(), None if dsum is None else dsum.data_ptr(), sum.data_ptr(),
           _float_vector(rstd, rows, "rstd"), _float_vector(gamma, cols, "gamma"), out.data_ptr(), gp, _devptr(workspace), workspace.numel())
     return out, dgamma
 
@@ -980,8 +1000,8 @@ def _byte_workspace(sizes, desc, workspace, like, stream):
 def patdnn_fp8_linear(x, x_scales, w, w_scales, bias=None, out=None, *, act="none", dtype=None, workspace=None, stream=None):
     """fp8 codes x [rows, in] times codes w [out, in], plus bias (float32 [out]), activated.  The weights' scales are of rows or of squares, as their shape
     says.  The result's type: ``out``'s or ``dtype``, float32 otherwise."""
-    torch = _torch()
-    _together(x, x_scales, w, w_scales, bias, out, workspace)
+    device = _together(x, x_scales, w, w_scales, bias, out, workspace)
+    torch = _modules["torch"]
     rows, cols, features, blocks, pointers = _fp8_operands(x, x_scales, ((w, w_scales),))
     if out is None:
         out = _new((rows, features), dtype or torch.float32, x, stream)
@@ -989,7 +1009,7 @@ def patdnn_fp8_linear(x, x_scales, w, w_scales, bias=None, out=None, *, act="non
         raise ValueError(f"output must be {(rows, features)}, of type dtype if that is given")
     desc = Fp8Desc(rows, cols, features, blocks, _type(out.dtype), _act(act), 0, _rows(out, "output"), 0)
     workspace, wp, size = _byte_workspace(lib().patdnn_fp8_linear_workspace_bytes, desc, workspace, x, stream)
-    _call(x, stream, lib().patdnn_fp8_linear, ctypes.byref(desc), *pointers, _float_vector(bias, features, "bias"), out.data_ptr(), wp, size)
+    _call(device, stream, lib().patdnn_fp8_linear, ctypes.byref(desc), *pointers, _float_vector(bias, features, "bias"), out.data_ptr(), wp, size)
     return out
 
 
@@ -997,36 +1017,31 @@ def patdnn_fp8_gated(x, x_scales, gate, gate_scales, up, up_scales, out=None, *,
                      stream=None):
     """act(x gate) * (x up) for fp8 codes x [rows, in] and gate, up [out, in]: values (of type ``out``'s or ``dtype``, float32 otherwise), or with
     ``fp8`` (codes, scales) of patdnn_fp8_quantize."""
-    torch = _torch()
-    _together(x, x_scales, gate, gate_scales, up, up_scales, out, scales, workspace)
+    device = _together(x, x_scales, gate, gate_scales, up, up_scales, out, scales, workspace)
     rows, cols, features, blocks, pointers = _fp8_operands(x, x_scales, ((gate, gate_scales), (up, up_scales)))
-    pieces = -(-features // 128)
-    shape = (rows, pieces * 128 if fp8 else features)
-    if fp8 and dtype is not None:
-        raise ValueError("dtype is for results that are no codes")
-    if not fp8 and scales is not None:
-        raise ValueError("scales are for codes")
-    if out is None:
-        out = _new(shape, torch.uint8 if fp8 else dtype or torch.float32, x, stream)
-    elif tuple(out.shape) != shape or (dtype and out.dtype != dtype):
-        raise ValueError(f"output must be {shape}, of type dtype if that is given")
     if fp8:
-        if scales is None:
-            scales = _new((rows, pieces), torch.uint8, x, stream)
-        op, kind, row = _byte_codes(out, "output"), PATDNN_FP8, 0
-        sp, _ = _byte_scales(scales, rows, pieces, "scales", 0)
+        if dtype is not None:
+            raise ValueError("dtype is for results that are no codes")
+        out, scales, op, sp = _new_codes(out, scales, rows, -(-features // 128), x, stream)
+        kind, row = PATDNN_FP8, 0
     else:
+        if scales is not None:
+            raise ValueError("scales are for codes")
+        if out is None:
+            out = _new((rows, features), dtype or _modules["torch"].float32, x, stream)
+        elif tuple(out.shape) != (rows, features) or (dtype and out.dtype != dtype):
+            raise ValueError(f"output must be {(rows, features)}, of type dtype if that is given")
         op, kind, row, sp = out.data_ptr(), _type(out.dtype), _rows(out, "output"), None
     desc = Fp8Desc(rows, cols, features, blocks, kind, _act(act), 0, row, 0)
     workspace, wp, size = _byte_workspace(lib().patdnn_fp8_gated_workspace_bytes, desc, workspace, x, stream)
-    _call(x, stream, lib().patdnn_fp8_gated, ctypes.byref(desc), *pointers, op, sp, wp, size)
+    _call(device, stream, lib().patdnn_fp8_gated, ctypes.byref(desc), *pointers, op, sp, wp, size)
     return (out, scales) if fp8 else out
 
 
 def patdnn_fp8_gated_backward(dh, x, x_scales, gate, gate_scales, up, up_scales, out=None, *, act="silu", dtype=None, workspace=None, stream=None):
     """Gradients of the two projections of patdnn_fp8_gated from dh [rows, out], the gradient of its result: [rows, 2 * out], gate's beside up's, of type ``out``'s,
     ``dtype`` or dh's."""
-    _together(x, x_scales, gate, gate_scales, up, up_scales, dh, out, workspace)
+    device = _together(x, x_scales, gate, gate_scales, up, up_scales, dh, out, workspace)
     rows, cols, features, blocks, pointers = _fp8_operands(x, x_scales, ((gate, gate_scales), (up, up_scales)))
     if tuple(dh.shape) != (rows, features):
         raise ValueError(f"dh must be {(rows, features)}")
@@ -1037,7 +1052,7 @@ def patdnn_fp8_gated_backward(dh, x, x_scales, gate, gate_scales, up, up_scales,
     desc = Fp8Desc(rows, cols, features, blocks, _type(out.dtype), _act(act), _type(dh.dtype), _rows(out, "output"), _rows(dh, "dh"))
     workspace, wp, size = _byte_workspace(lib().patdnn_fp8_gated_backward_workspace_bytes, desc, workspace, x, stream)
     at = out.data_ptr()
-    _call(x, stream, lib().patdnn_fp8_gated_backward, ctypes.byref(desc), dh.data_ptr(), *pointers, at, at + features * out.element_size(), wp, size)
+    _call(device, stream, lib().patdnn_fp8_gated_backward, ctypes.byref(desc), dh.data_ptr(), *pointers, at, at + features * out.element_size(), wp, size)
     return out
 
 

@@ -67,6 +67,7 @@ __device__ __forceinline__ void load_values(const void* from, long long at, int 
 
 // Many rows (kernel_fp8_tiles.hip).
 bool product_tiles_fit(const ProductShape& s);
-hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, hipStream_t stream);
+size_t product_tiles_workspace_bytes(const ProductShape& s);
+hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, float* partial, hipStream_t stream);
 
 }  // namespace patdnn

@@ -97,9 +97,18 @@ hipError_t launch_rows(const ProductShape& s, const ProductTensors& t, hipStream
 }
 
 // Whether the call is for this kernel and not for tiles.
-bool by_rows(const ProductShape& s) { return s.rows <= kRows || !product_tiles_fit(s); }
+#ifdef FP8_TUNE
+extern "C" int patdnn_tune_fp8[4];
+#endif
+bool by_rows(const ProductShape& s)
+{
+#ifdef FP8_TUNE
+    if (patdnn_tune_fp8[3]) return patdnn_tune_fp8[3] == 1;
+#endif
+    return s.rows <= kRows || !product_tiles_fit(s);
+}
 
-// The workspace: h in fp32, where codes are made of it by a launch of their own.
+// The workspace: slices' sums of the tiles; h in fp32, where codes are made of it by a launch of their own.
 bool codes_apart(const ProductShape& s) { return s.kind == kGated && s.out_type == kFp8 && by_rows(s); }
 
 }  // namespace
@@ -111,11 +120,14 @@ bool product_fits(const ProductShape& s)
            (!codes_apart(s) || fp8_fits(Fp8Shape{s.rows, s.out, kF32, false, false, s.out}, true));
 }
 
-size_t product_workspace_bytes(const ProductShape& s) { return codes_apart(s) ? (size_t)s.rows * (size_t)s.out * 4 : 0; }
+size_t product_workspace_bytes(const ProductShape& s)
+{
+    return !by_rows(s) ? product_tiles_workspace_bytes(s) : codes_apart(s) ? (size_t)s.rows * (size_t)s.out * 4 : 0;
+}
 
 hipError_t launch_product(const ProductShape& shape, const ProductTensors& tensors, void* workspace, hipStream_t stream)
 {
-    if (!by_rows(shape)) return launch_product_tiles(shape, tensors, stream);
+    if (!by_rows(shape)) return launch_product_tiles(shape, tensors, static_cast<float*>(workspace), stream);
     ProductShape s = shape;
     ProductTensors t = tensors;
     const bool apart = codes_apart(s), exact = s.out_type == kF32;

@@ -20,9 +20,10 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 struct Args {
     ProductShape s;
     ProductTensors t;
+    float* partial;                                      // [slice][row][sums], of calls in slices
     int pieces;                                          // stages
-    int tiles_n, tiles_m;
-    FastDiv by_band, by_last;                            // tiles of a band, rows of tiles of the last band
+    int tiles_n, tiles_m, slices, slice_pieces;          // slices of k
+    FastDiv by_tiles, by_band, by_last;                  // tiles of a slice, of a band, rows of tiles of the last band
 };
 constexpr int kBand = 8;                                 // rows of tiles that are taken side by side
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -95,16 +96,18 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
     const int r = lane & 15, kb = lane >> 4;
     // Which tile: workgroups go to the eight XCDs in turn, each takes a run of tiles, kBand rows of them at a time.
-    int tn, tm;
+    int slice, tn, tm;
     {
-        const int all = A.tiles_n * A.tiles_m, xcd = (int)blockIdx.x & 7, q = all >> 3, rest = all & 7;
-        const int t = xcd * q + min(xcd, rest) + ((int)blockIdx.x >> 3);
+        const int tiles = A.tiles_n * A.tiles_m, all = tiles * A.slices, xcd = (int)blockIdx.x & 7, q = all >> 3, rest = all & 7;
+        int t = xcd * q + min(xcd, rest) + ((int)blockIdx.x >> 3);
+        slice = uniform((int)fast_div((uint32_t)t, A.by_tiles));
+        t -= slice * tiles;
         const int band = uniform((int)fast_div((uint32_t)t, A.by_band)), in_band = t - band * kBand * A.tiles_n, height = min(kBand, A.tiles_m - band * kBand);
         tn = uniform(height == kBand ? in_band / kBand : (int)fast_div((uint32_t)in_band, A.by_last));
         tm = band * kBand + in_band - tn * height;
     }
-    const int n0 = tn * kOut, m0 = tm * BM, pieces = A.pieces;
-    const long long pitch = (long long)pieces * 128;
+    const int n0 = tn * kOut, m0 = tm * BM, first_piece = slice * A.slice_pieces, pieces = min(A.slice_pieces, A.pieces - first_piece);
+    const long long pitch = (long long)A.pieces * 128;
 
     // A row of LDS: whose it is (0, 1: of the weights; 2: of x), and which row behind the tile's first.  Rows past the end are those of the last one.
     auto side_of = [&](int row) { return row >= BN ? 2 : kTwo ? row >> 6 & 1 : 0; };
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
 #pragma unroll
     for (int i = 0; i < S::kFetches; ++i) {
         const int first = fetch_row + i * 8, side = side_of(first);
-        const uint8_t* p = side == 2 ? A.t.x + m0 * pitch : (kTwo && side == 1 ? A.t.w2 : A.t.w) + n0 * pitch;
+        const uint8_t* p = (side == 2 ? A.t.x + m0 * pitch : (kTwo && side == 1 ? A.t.w2 : A.t.w) + n0 * pitch) + first_piece * 128;
         low[i] = uniform((int)(uint32_t)(uint64_t)p);
         high[i] = uniform((int)((uint64_t)p >> 32 & 0xffff));
         row_at[i] = uniform(row_of(first) * (int)pitch);
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
         const int row = min(k * S::kThreads + (int)threadIdx.x, S::kRows - 1), side = side_of(row);
         const uint8_t* from = side == 2 ? A.t.x_scales : kTwo && side == 1 ? A.t.w2_scales : A.t.w_scales;
         const int at = side == 2 ? m0 + min(row_of(row), x_last) : n0 + min(row_of(row), w_last);
-        scales_at[k] = from + (long long)(side != 2 && A.s.squares ? at >> 7 : at) * pieces;
+        scales_at[k] = from + (long long)(side != 2 && A.s.squares ? at >> 7 : at) * A.pieces + first_piece;
     }
     uint32_t words[S::kWords];
     // (four bytes that lie in the row: in its last group those before it come along, and are shifted out)
@@ -337,6 +340,22 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     for (int g = 0; g < kGroups; ++g) {
         const int n = n0 + wn * (kOut / WN) + g * 64 + kb * 16, left = A.s.out - n;
         float add[16];
+        if (A.slices > 1) {
+            float* to = A.partial + ((long long)slice * A.s.rows + m0) * (kTwo ? 2ll : 1ll) * A.s.out + n;
+#pragma unroll
+            for (int j = 0; j < S::kTM; ++j) {
+                const int m = wm * (16 * S::kTM) + j * 16 + r;
+                if (m0 + m >= A.s.rows || left <= 0) continue;
+#pragma unroll
+                for (int side = 0; side < (kTwo ? 2 : 1); ++side) {
+                    float z[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = acc[(g + side) * 4 + i / 4][j][i % 4];
+                    store_results(to, ((long long)m * (kTwo ? 2 : 1) + side) * A.s.out, kF32, left, z);
+                }
+            }
+            continue;
+        }
         if (KIND == kLinear)
 #pragma unroll
             for (int i = 0; i < 16; ++i) add[i] = A.t.bias && i < left ? A.t.bias[n + i] : 0.0f;
@@ -415,6 +434,42 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     }
 }
 
+// Adds the slices up in their order, and makes the results: 256 outputs of a row a workgroup.
+template <int KIND>
+__global__ __launch_bounds__(256) void product_join_kernel(ProductShape s, ProductTensors t, const float* __restrict__ partial, int slices, FastDiv by_out_blocks)
+{
+    constexpr int kSides = KIND == kLinear ? 1 : 2;
+    __shared__ uint32_t tops[4];
+    const uint32_t m = fast_div(blockIdx.x, by_out_blocks);
+    const int n = (int)(blockIdx.x - m * (uint32_t)((s.out + 255) / 256)) * 256 + (int)threadIdx.x;
+    const long long stride = (long long)s.rows * kSides * s.out;
+    float z[2] = {0.0f, 0.0f};
+    if (n < s.out) {
+        const float* p = partial + (long long)m * kSides * s.out + n;
+#pragma unroll 4
+        for (int k = 0; k < slices; ++k)
+#pragma unroll
+            for (int i = 0; i < kSides; ++i) z[i] += p[k * stride + i * s.out];
+    }
+    if (KIND == kGated && s.out_type == kFp8) {
+        const float h = n < s.out ? activate_as(z[0], s.act) * z[1] : 0.0f;
+        uint32_t top = largest_of_16_lanes(__float_as_uint(h) & 0x7fffffffu);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+        const int wave = (int)threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) tops[wave] = top;
+        __syncthreads();
+        const int pieces = (s.out + 127) / 128;
+        if (n >= pieces * 128) return;
+        const uint32_t byte = fp8_scale_byte(max(tops[wave], tops[wave ^ 1]));
+        const uint32_t code = byte == kNanScale ? 0u : fp8_encode4(h, 0.0f, 0.0f, 0.0f, fp8_inverse(byte));
+        static_cast<uint8_t*>(t.out)[(long long)m * pieces * 128 + n] = (uint8_t)code;
+        if (n % 128 == 0) t.out_scales[(long long)m * pieces + n / 128] = (uint8_t)byte;
+    } else if (n < s.out) {
+        finish_one<KIND>(s, t, (int)m, n, z[0], z[1]);
+    }
+}
+
 template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS>
 hipError_t launch_shape(Args A, hipStream_t stream)
 {
@@ -422,17 +477,63 @@ hipError_t launch_shape(Args A, hipStream_t stream)
     constexpr int kOut = KIND == kLinear ? BN : BN / 2;
     A.tiles_n = (A.s.out + kOut - 1) / kOut;
     A.tiles_m = (A.s.rows + BM - 1) / BM;
+    A.by_tiles = make_fast_div((uint32_t)(A.tiles_n * A.tiles_m));
     A.by_band = make_fast_div((uint32_t)(kBand * A.tiles_n));
     A.by_last = make_fast_div((uint32_t)(A.tiles_m % kBand ? A.tiles_m % kBand : kBand));
     static std::atomic<uint64_t> allowed{0};
     const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS>), allowed);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS>), dim3((unsigned)(A.tiles_n * A.tiles_m)), dim3(S::kThreads), S::kLds, stream, A);
+    hipLaunchKernelGGL((product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS>), dim3((unsigned)(A.tiles_n * A.tiles_m * A.slices)), dim3(S::kThreads), S::kLds,
+                       stream, A);
+    if (const hipError_t launched = hipGetLastError(); launched != hipSuccess || A.slices == 1) return launched;
+    const int across = (A.s.out + 255) / 256;
+    hipLaunchKernelGGL((product_join_kernel<KIND>), dim3((unsigned)((long long)across * A.s.rows)), dim3(256), 0, stream, A.s, A.t, A.partial, A.slices,
+                       make_fast_div((uint32_t)across));
     return hipGetLastError();
 }
 
 // Tiles of bn outputs x bm rows.
 long long tiles_of(const ProductShape& s, int bn, int bm) { return ceil_div(s.out, bn) * ceil_div(s.rows, bm); }
+
+// The shape, outputs x rows, and slices of k of a call.
+struct Plan {
+    int outputs, rows, slices, slice_pieces;
+};
+#ifdef FP8_TUNE
+}
+}
+extern "C" int patdnn_tune_fp8[4] = {0, 0, 0, 0};
+namespace patdnn {
+namespace {
+#endif
+Plan plan_of(const ProductShape& s)
+{
+    const bool exact = s.out_type == kF32;
+    const int pieces = (int)fp8_pieces(s.in);
+    // The largest tiles that three of four CUs get one of (256 x 4096 -> 12288, 192 tiles of 128^2: 26.5 us, 32 with 64^2; 512 x 4096 -> 4096, 128 of them: 25.9
+    // and 19.5; gated 512 x 4096 -> 12288, 192 of 256 rows: 75 and 83).  Results in fp32 stop at 128 rows, which the gated pair's reach with fewer where k is
+    // long enough to be cut (256 x 12288 -> 4096, 64 tiles: 65 us, 76 with 64 rows; backward 777 x 1500 -> 2100, 119 tiles: 35 us, 25 with 64 rows).
+    constexpr long long kEnough = 192;
+    Plan p{};
+    if (s.kind == kLinear)
+        p = !exact && tiles_of(s, 256, 256) >= kEnough ? Plan{256, 256} : tiles_of(s, 128, 128) >= kEnough ? Plan{128, 128} : Plan{64, 64};
+    else if (exact) p = tiles_of(s, 128, 128) >= (pieces >= 64 ? 64 : kEnough) ? Plan{128, 128} : Plan{128, 64};
+    else p = tiles_of(s, 128, 256) >= kEnough ? Plan{128, 256} : Plan{128, 64};
+    // Fewer tiles than CUs are cut along k, into slices of eight stages and more (four in fp32, whose take longer): adding them up is a launch of its own, whose
+    // bytes cost what it saves where there are many rows (us in 1, 2, 4 and 8 slices: 32 x 4096 -> 4096 14.8, 12.3, 11.0, 12.5; 128 x 4096 -> 4096 15.1, 14.9, 17.0,
+    // 22.7; 64 x 12288 -> 4096 36, 23, 17.7, 17.7; gated 256 x 12288 -> 4096 77, 54, 62, 89).  Linear layers' long slices pay up to twice as many (256 x 12288 ->
+    // 4096 37, 33, 37).
+    const long long tiles = tiles_of(s, p.outputs, p.rows);
+    long long slices = std::max<long long>(1, std::min<long long>(pieces / (exact ? 4 : 8), 256 / tiles));
+    if (s.kind == kLinear) slices = std::max<long long>(slices, std::min<long long>(pieces / 24, 512 / tiles));
+#ifdef FP8_TUNE
+    if (patdnn_tune_fp8[0]) p.outputs = patdnn_tune_fp8[0], p.rows = patdnn_tune_fp8[1];
+    if (patdnn_tune_fp8[2]) slices = std::min(pieces, patdnn_tune_fp8[2]);
+#endif
+    p.slice_pieces = (int)((pieces + slices - 1) / slices);
+    p.slices = (pieces + p.slice_pieces - 1) / p.slice_pieces;
+    return p;
+}
 
 }  // namespace
 
@@ -442,20 +543,33 @@ bool product_tiles_fit(const ProductShape& s)
     return fp8_pieces(s.in) * 128 * 256 <= INT32_MAX && tiles_of(s, 64, 64) <= kMostBlocks / 4;
 }
 
-hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, hipStream_t stream)
+size_t product_tiles_workspace_bytes(const ProductShape& s)
 {
-    Args A{s, t, (int)fp8_pieces(s.in), 0, 0, {}, {}};
+    const Plan p = plan_of(s);
+    return p.slices > 1 ? (size_t)p.slices * (size_t)s.rows * (size_t)s.out * (s.kind == kLinear ? 4 : 8) : 0;
+}
+
+hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, float* partial, hipStream_t stream)
+{
+    const Plan p = plan_of(s);
+    Args A{};
+    A.s = s;
+    A.t = t;
+    A.partial = partial;
+    A.pieces = (int)fp8_pieces(s.in);
+    A.slices = p.slices;
+    A.slice_pieces = p.slice_pieces;
     const bool exact = s.out_type == kF32;
     if (s.kind == kLinear) {
-        if (exact) return tiles_of(s, 128, 128) >= 256 ? launch_shape<kLinear, true, 128, 128, 2, 2, 2>(A, stream) : launch_shape<kLinear, true, 64, 64, 1, 4, 2>(A, stream);
-        return tiles_of(s, 256, 256) >= 256   ? launch_shape<kLinear, false, 256, 256, 2, 4, 2>(A, stream)
-               : tiles_of(s, 128, 128) >= 256 ? launch_shape<kLinear, false, 128, 128, 2, 2, 2>(A, stream)
-                                              : launch_shape<kLinear, false, 64, 64, 1, 4, 4>(A, stream);
+        if (exact) return p.rows == 128 ? launch_shape<kLinear, true, 128, 128, 2, 2, 2>(A, stream) : launch_shape<kLinear, true, 64, 64, 1, 4, 2>(A, stream);
+        return p.rows == 256   ? launch_shape<kLinear, false, 256, 256, 2, 4, 2>(A, stream)
+               : p.rows == 128 ? launch_shape<kLinear, false, 128, 128, 2, 2, 2>(A, stream)
+                               : launch_shape<kLinear, false, 64, 64, 1, 4, 4>(A, stream);
     }
     auto run = [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
-        if (exact) return tiles_of(s, 128, 128) >= 256 ? launch_shape<KIND, true, 256, 128, 2, 4, 2>(A, stream) : launch_shape<KIND, true, 256, 64, 2, 4, 2>(A, stream);
-        return tiles_of(s, 128, 256) >= 256 ? launch_shape<KIND, false, 256, 256, 2, 4, 2>(A, stream) : launch_shape<KIND, false, 256, 64, 2, 4, 2>(A, stream);
+        if (exact) return p.rows == 128 ? launch_shape<KIND, true, 256, 128, 2, 4, 2>(A, stream) : launch_shape<KIND, true, 256, 64, 2, 4, 2>(A, stream);
+        return p.rows == 256 ? launch_shape<KIND, false, 256, 256, 2, 4, 2>(A, stream) : launch_shape<KIND, false, 256, 64, 2, 4, 2>(A, stream);
     };
     return s.kind == kGated ? run(Const<kGated>{}) : run(Const<kGatedBackward>{});
 }

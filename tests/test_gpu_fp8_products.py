@@ -204,8 +204,9 @@ def test_graph_and_no_rows(torch):
     assert B.patdnn_fp8_gated_backward(x[:0, :200], xc[:0], xs[:0], gc, gs, uc, us).shape == (0, 400)
 
 
-# (sizes that take each tile shape, with rows and outputs that end inside a tile, and k of one to nine stages)
-LARGE = [(4090, 300, 4100), (2100, 520, 2000), (520, 1100, 700), (8200, 128, 2050), (300, 1030, 33000)]
+# (sizes that take each tile shape, with rows and outputs that end inside a tile, and k of one to nine stages; and slices of k, of eight pieces and more, the last of
+# three)
+LARGE = [(4090, 300, 4100), (2100, 520, 2000), (520, 1100, 700), (8200, 128, 2050), (300, 1030, 33000), (40, 5000, 300), (70, 4100, 1000), (20, 7200, 130)]
 
 
 def whole(torch, rows, k, squares, seed):

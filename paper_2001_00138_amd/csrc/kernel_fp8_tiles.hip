@@ -25,6 +25,7 @@ struct Args {
     int tiles_n, tiles_m, slices, slice_pieces;          // slices of k
     FastDiv by_tiles, by_band, by_last;                  // tiles of a slice, of a band, rows of tiles of the last band
 };
+constexpr int kGatedCodes = 3;                          // kGated with codes as its result
 constexpr int kBand = 8;                                 // rows of tiles that are taken side by side
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -85,7 +86,8 @@ struct Tile {
     static_assert(NS == 2 || NS == 4, "stages by their place in a group of four");
 };
 
-template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS>
+// SLICED: sums of a slice of k go to A.partial.
+template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS, bool SLICED>
 __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
 {
     using S = Tile<BN, BM, WN, WM, NS>;
@@ -96,17 +98,20 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
     const int r = lane & 15, kb = lane >> 4;
     // Which tile: workgroups go to the eight XCDs in turn, each takes a run of tiles, kBand rows of them at a time.
-    int slice, tn, tm;
+    int slice = 0, tn, tm;
     {
-        const int tiles = A.tiles_n * A.tiles_m, all = tiles * A.slices, xcd = (int)blockIdx.x & 7, q = all >> 3, rest = all & 7;
+        const int tiles = A.tiles_n * A.tiles_m, all = SLICED ? tiles * A.slices : tiles, xcd = (int)blockIdx.x & 7, q = all >> 3, rest = all & 7;
         int t = xcd * q + min(xcd, rest) + ((int)blockIdx.x >> 3);
-        slice = uniform((int)fast_div((uint32_t)t, A.by_tiles));
-        t -= slice * tiles;
+        if (SLICED) {
+            slice = uniform((int)fast_div((uint32_t)t, A.by_tiles));
+            t -= slice * tiles;
+        }
         const int band = uniform((int)fast_div((uint32_t)t, A.by_band)), in_band = t - band * kBand * A.tiles_n, height = min(kBand, A.tiles_m - band * kBand);
         tn = uniform(height == kBand ? in_band / kBand : (int)fast_div((uint32_t)in_band, A.by_last));
         tm = band * kBand + in_band - tn * height;
     }
-    const int n0 = tn * kOut, m0 = tm * BM, first_piece = slice * A.slice_pieces, pieces = min(A.slice_pieces, A.pieces - first_piece);
+    const int n0 = tn * kOut, m0 = tm * BM, first_piece = SLICED ? slice * A.slice_pieces : 0;
+    const int pieces = SLICED ? min(A.slice_pieces, A.pieces - first_piece) : A.pieces;
     const long long pitch = (long long)A.pieces * 128;
 
     // A row of LDS: whose it is (0, 1: of the weights; 2: of x), and which row behind the tile's first.  Rows past the end are those of the last one.
@@ -340,7 +345,7 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     for (int g = 0; g < kGroups; ++g) {
         const int n = n0 + wn * (kOut / WN) + g * 64 + kb * 16, left = A.s.out - n;
         float add[16];
-        if (A.slices > 1) {
+        if constexpr (SLICED) {
             float* to = A.partial + ((long long)slice * A.s.rows + m0) * (kTwo ? 2ll : 1ll) * A.s.out + n;
 #pragma unroll
             for (int j = 0; j < S::kTM; ++j) {
@@ -359,13 +364,14 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
         if (KIND == kLinear)
 #pragma unroll
             for (int i = 0; i < 16; ++i) add[i] = A.t.bias && i < left ? A.t.bias[n + i] : 0.0f;
-        if (KIND == kGated && A.s.out_type == kFp8) {
+        if constexpr (KIND == kGatedCodes) {
             // the largest of a row's 128 outputs is that of its lanes in the two wavefronts that have them
-            static_assert(!kTwo || WN == 2, "128 outputs in two wavefronts");
+            static_assert(WN == 2, "128 outputs in two wavefronts");
             uint32_t* tops = reinterpret_cast<uint32_t*>(lds);           // [wn][row]
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < S::kTM; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
                 uint32_t top = 0;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -381,6 +387,7 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             const int out_pieces = (A.s.out + 127) / 128;
 #pragma unroll
             for (int j = 0; j < S::kTM; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
                 const int at = wm * (16 * S::kTM) + j * 16 + r, m = m0 + at;
                 if (m >= A.s.rows) continue;
                 const uint32_t byte = fp8_scale_byte(max(tops[at], tops[BM + at]));
@@ -399,6 +406,7 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
         }
 #pragma unroll
         for (int j = 0; j < S::kTM; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
             const int m = m0 + wm * (16 * S::kTM) + j * 16 + r;
             if (m >= A.s.rows || left <= 0) continue;
             float z[16], y[16];
@@ -451,7 +459,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductShape s, Produ
 #pragma unroll
             for (int i = 0; i < kSides; ++i) z[i] += p[k * stride + i * s.out];
     }
-    if (KIND == kGated && s.out_type == kFp8) {
+    if constexpr (KIND == kGatedCodes) {
         const float h = n < s.out ? activate_as(z[0], s.act) * z[1] : 0.0f;
         uint32_t top = largest_of_16_lanes(__float_as_uint(h) & 0x7fffffffu);
         top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
@@ -480,12 +488,19 @@ hipError_t launch_shape(Args A, hipStream_t stream)
     A.by_tiles = make_fast_div((uint32_t)(A.tiles_n * A.tiles_m));
     A.by_band = make_fast_div((uint32_t)(kBand * A.tiles_n));
     A.by_last = make_fast_div((uint32_t)(A.tiles_m % kBand ? A.tiles_m % kBand : kBand));
-    static std::atomic<uint64_t> allowed{0};
-    const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS>), allowed);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS>), dim3((unsigned)(A.tiles_n * A.tiles_m * A.slices)), dim3(S::kThreads), S::kLds,
-                       stream, A);
-    if (const hipError_t launched = hipGetLastError(); launched != hipSuccess || A.slices == 1) return launched;
+    auto launch = [&](auto sliced) {
+        constexpr auto kernel = product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS, decltype(sliced)::value != 0>;
+        static std::atomic<uint64_t> allowed{0};
+        if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(kernel), allowed); e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(A.tiles_n * A.tiles_m * A.slices)), dim3(S::kThreads), S::kLds, stream, A);
+        return hipGetLastError();
+    };
+    // (the largest tiles are taken where there are enough of them)
+    if constexpr (BM < 256) {
+        if (A.slices > 1)
+            if (const hipError_t e = launch(Const<1>{}); e != hipSuccess) return e;
+    }
+    if (A.slices == 1) return launch(Const<0>{});
     const int across = (A.s.out + 255) / 256;
     hipLaunchKernelGGL((product_join_kernel<KIND>), dim3((unsigned)((long long)across * A.s.rows)), dim3(256), 0, stream, A.s, A.t, A.partial, A.slices,
                        make_fast_div((uint32_t)across));
@@ -529,6 +544,7 @@ Plan plan_of(const ProductShape& s)
 #ifdef FP8_TUNE
     if (patdnn_tune_fp8[0]) p.outputs = patdnn_tune_fp8[0], p.rows = patdnn_tune_fp8[1];
     if (patdnn_tune_fp8[2]) slices = std::min(pieces, patdnn_tune_fp8[2]);
+    if (p.rows == 256) slices = 1;
 #endif
     p.slice_pieces = (int)((pieces + slices - 1) / slices);
     p.slices = (pieces + p.slice_pieces - 1) / p.slice_pieces;
@@ -568,10 +584,11 @@ hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, 
     }
     auto run = [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
-        if (exact) return p.rows == 128 ? launch_shape<KIND, true, 256, 128, 2, 4, 2>(A, stream) : launch_shape<KIND, true, 256, 64, 2, 4, 2>(A, stream);
+        if constexpr (KIND != kGatedCodes)
+            if (exact) return p.rows == 128 ? launch_shape<KIND, true, 256, 128, 2, 4, 2>(A, stream) : launch_shape<KIND, true, 256, 64, 2, 4, 2>(A, stream);
         return p.rows == 256 ? launch_shape<KIND, false, 256, 256, 2, 4, 2>(A, stream) : launch_shape<KIND, false, 256, 64, 2, 4, 2>(A, stream);
     };
-    return s.kind == kGated ? run(Const<kGated>{}) : run(Const<kGatedBackward>{});
+    return s.kind == kGatedBackward ? run(Const<kGatedBackward>{}) : s.out_type == kFp8 ? run(Const<kGatedCodes>{}) : run(Const<kGated>{});
 }
 
 }  // namespace patdnn

@@ -289,8 +289,8 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             read_scales(t + 1);
         };
         if (S::kTM > 1) read_b(F ^ 1);
+        read_a(1, 0);
         if constexpr (EXACT) {
-            read_a(1, 0);
             read_a(1, 1);
             widen_b(F);
             if (S::kTM > 1) widen_b(F ^ 1);
@@ -306,18 +306,17 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             phase();
             if (S::kTM > 1) multiply(0, 0, F ^ 1);
             phase();
-            read_a(1, 0);
             read_a(1, 1);
             if (S::kTM > 1) multiply(0, 1, F ^ 1);
             phase();
             next_stage();
+            read_a(0, 0);
             if (S::kTM > 1) {
                 multiply(1, 0, F ^ 1);
                 multiply(1, 1, F ^ 1);
             }
             phase();
             read_b(F ^ 1);
-            read_a(0, 0);
             multiply(1, 0, F);
             phase();
             read_a(0, 1);

@@ -6,21 +6,27 @@
 
 namespace patdnn {
 
-// Gradients of the two projections g and u from that of h = act(g) u.  SiLU's slope is s (1 + z (1 - s)) with s = 1 / (1 + exp(-z)), and 0
-// where s is.
-__device__ __forceinline__ void gated_gradients(float g, float u, float dh, int act, float& dg, float& du)
+// Gradients of the two projections g and u from that of h = act(g) u.  SiLU's slope, with s = 1 / (1 + exp(-z)), is s (1 + z (1 - s)) = s + z s (1 - s).
+template <int ACT>
+__device__ __forceinline__ void gated_gradients(float g, float u, float dh, float& dg, float& du)
 {
     float value = g, slope = 1.0f;
-    if (act == kActRelu) {
+    if (ACT == kActRelu) {
         value = activate<kActRelu>(g);
         slope = g <= 0.0f ? 0.0f : 1.0f;
-    } else if (act == kActSilu) {
+    } else if (ACT == kActSilu) {
         const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
         value = g * s;
-        slope = s == 0.0f ? 0.0f : s * (1.0f + g * (1.0f - s));
+        slope = s + value * (1.0f - s);
     }
     dg = dh * u * slope;
     du = dh * value;
+}
+__device__ __forceinline__ void gated_gradients_as(int act, float g, float u, float dh, float& dg, float& du)
+{
+    if (act == kActSilu) gated_gradients<kActSilu>(g, u, dh, dg, du);
+    else if (act == kActRelu) gated_gradients<kActRelu>(g, u, dh, dg, du);
+    else gated_gradients<kActNone>(g, u, dh, dg, du);
 }
 __device__ __forceinline__ float load_as(const void* from, long long at, int type)
 {
@@ -40,29 +46,10 @@ __device__ __forceinline__ void finish_one(const ProductShape& s, const ProductT
         store_as(t.out, at, s.out_type, activate_as(a, s.act) * b);
     } else {
         float dg, du;
-        gated_gradients(a, b, load_as(t.dh, m * s.dh_row + n, s.dh_type), s.act, dg, du);
+        gated_gradients_as(s.act, a, b, load_as(t.dh, m * s.dh_row + n, s.dh_type), dg, du);
         store_as(t.out, at, s.out_type, dg);
         store_as(t.out2, at, s.out_type, du);
     }
-}
-
-// Sixteen neighbouring values of a row, `left` of them inside it.
-template <class T>
-__device__ __forceinline__ void load_sixteen(const void* from, long long at, int left, float (&z)[16])
-{
-#pragma unroll
-    for (int i = 0; i < 16; i += 8) {
-        float v[8];
-        load8_floats(static_cast<const T*>(from) + at + i, left - i, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[i + e] = v[e];
-    }
-}
-__device__ __forceinline__ void load_values(const void* from, long long at, int type, int left, float (&z)[16])
-{
-    if (type == kF32) load_sixteen<float>(from, at, left, z);
-    else if (type == kF16) load_sixteen<_Float16>(from, at, left, z);
-    else load_sixteen<__bf16>(from, at, left, z);
 }
 
 // Many rows (kernel_fp8_tiles.hip).

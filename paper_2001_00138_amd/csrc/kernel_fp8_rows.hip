@@ -6,14 +6,19 @@
 //
 // The weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs (of both projections); its wavefronts take
 // pieces of 128 values of k in turn, straight from memory to registers, and add their sums up in LDS, in their order.
+//
+// From memory: 1 x 12288 -> 4096 12.7 us, 4.0 TB/s of weights; gated 1 x 4096 -> 12288 21.9 us, 4.6 TB/s.
 #include "fp8_products.hpp"
 
+#ifdef FP8_TUNE
+extern "C" int patdnn_tune_fp8[4];
+#endif
 namespace patdnn {
 
 namespace {
 
 constexpr int kRows = 16;                                // rows of x a workgroup
-constexpr int kAhead = 2;                                // pieces of weights that a wavefront asks for together
+constexpr int kAhead = 2;                                // pieces of weights that a wavefront asks for together (one to four are alike)
 
 struct Args {
     ProductShape s;
@@ -96,16 +101,17 @@ hipError_t launch_rows(const ProductShape& s, const ProductTensors& t, hipStream
     return hipGetLastError();
 }
 
-// Whether the call is for this kernel and not for tiles.
-#ifdef FP8_TUNE
-extern "C" int patdnn_tune_fp8[4];
-#endif
+// Whether the call is for this kernel and not for tiles: up to 16 rows, but from nine on tiles read x less often where there are many weights and the sums are the fp8
+// instruction's (16 rows, us here and in tiles: 12288 -> 4096 16.3 and 14.4, 4096 -> 12288 16.3 and 14.7, gated 24.5 and 22.8; 8 rows 13.1 and 14.2; 16 x 4096 -> 4096 7.8
+// and 10.4; results in fp32 16.3 and 16.7).
 bool by_rows(const ProductShape& s)
 {
 #ifdef FP8_TUNE
     if (patdnn_tune_fp8[3]) return patdnn_tune_fp8[3] == 1;
 #endif
-    return s.rows <= kRows || !product_tiles_fit(s);
+    if (!product_tiles_fit(s)) return true;
+    const long long weights = (long long)s.in * s.out * (s.kind == kLinear ? 1 : 2);
+    return s.rows <= 8 || (s.rows <= kRows && (s.out_type == kF32 || weights < 48ll << 20));
 }
 
 // The workspace: slices' sums of the tiles; h in fp32, where codes are made of it by a launch of their own.

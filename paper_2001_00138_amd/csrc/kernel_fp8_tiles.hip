@@ -86,8 +86,8 @@ struct Tile {
     static_assert(NS == 2 || NS == 4, "stages by their place in a group of four");
 };
 
-// SLICED: sums of a slice of k go to A.partial.
-template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS, bool SLICED>
+// SLICED: sums of a slice of k go to A.partial.  D: dh's type.  (What is decided here and not in the kernel is what would cost it registers.)
+template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS, bool SLICED, class D>
 __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
 {
     using S = Tile<BN, BM, WN, WM, NS>;
@@ -114,37 +114,28 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     const int pieces = SLICED ? min(A.slice_pieces, A.pieces - first_piece) : A.pieces;
     const long long pitch = (long long)A.pieces * 128;
 
-    // A row of LDS: whose it is (0, 1: of the weights; 2: of x), and which row behind the tile's first.  Rows past the end are those of the last one.
+    // A row of LDS: whose it is (0, 1: of the weights; 2: of x), and which row behind the tile's first.
     auto side_of = [&](int row) { return row >= BN ? 2 : kTwo ? row >> 6 & 1 : 0; };
     auto row_of = [&](int row) { return row >= BN ? row - BN : kTwo ? (row >> 7) * 64 + (row & 63) : row; };
     const int w_last = A.s.out - 1 - n0, x_last = A.s.rows - 1 - m0;
-    const int fetch_row = wave * S::kFetches * 8;                        // this wavefront's first row
-    const uint32_t w_end = (uint32_t)(w_last * (int)pitch), x_end = (uint32_t)(x_last * (int)pitch);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-    // of each fetch, in scalar registers: where its side's rows begin, how far behind that its eight and the side's last one are
-    int low[S::kFetches], high[S::kFetches], row_at[S::kFetches], end_at[S::kFetches];
-#pragma unroll
-    for (int i = 0; i < S::kFetches; ++i) {
-        const int first = fetch_row + i * 8, side = side_of(first);
-        const uint8_t* p = (side == 2 ? A.t.x + m0 * pitch : (kTwo && side == 1 ? A.t.w2 : A.t.w) + n0 * pitch) + first_piece * 128;
-        low[i] = uniform((int)(uint32_t)(uint64_t)p);
-        high[i] = uniform((int)((uint64_t)p >> 32 & 0xffff));
-        row_at[i] = uniform(row_of(first) * (int)pitch);
-        end_at[i] = uniform((int)(side == 2 ? x_end : w_end));
-    }
-    auto fetch_stage = [&](int t) {
-        // (the lane's offsets are made again each time: eight registers of them would be spilled)
-        int l = lane;
-        asm volatile("" : "+v"(l));
-        const uint32_t lane_at = (uint32_t)((l >> 3) * (int)pitch);
-#pragma unroll
-        for (int i = 0; i < S::kFetches; ++i) {
-            const int first = fetch_row + i * 8;
-            const uint32_t row = min(lane_at + (uint32_t)row_at[i], (uint32_t)end_at[i]);
-            const int mask = first < BN ? 3 : 7, more = first < BN ? (first >> 4 & 1) << 2 : 0;
-            fetch16(intx4{low[i], high[i], -1, 0x00020000}, lds0 + (uint32_t)uniform((t & (NS - 1)) * S::kStage + first * 128),
-                    row + (uint32_t)(((l & 7) ^ ((l >> 3 & mask) | more)) * 16), (uint32_t)min(t, pieces - 1) * 128);
-        }
+    // The wavefronts fetch eight rows each, of one side, and so on.  What lies past a side's end the buffer's own check keeps from being read (it compares a lane's part of the
+    // offset with what the scalar part leaves, which is never past the last row); what stands in LDS there reaches only results that are dropped.
+    constexpr int kTogether = 8 * S::kWaves;
+    static_assert(BN % kTogether == 0 && BM % kTogether == 0 && (!kTwo || kTogether == 64), "rows that are fetched together are of one side");
+    auto buffer_of_side = [&](int side) {
+        const uint64_t p = (uint64_t)((side == 2 ? A.t.x + m0 * pitch : (side == 1 ? A.t.w2 : A.t.w) + n0 * pitch) + first_piece * 128);
+        const long long bytes = ((long long)(side == 2 ? x_last : w_last) + 1) * pitch - first_piece * 128;
+        return intx4{uniform((int)(uint32_t)p), uniform((int)(p >> 32 & 0xffff)), uniform((int)(uint32_t)min(bytes, 0xffffffffll)), 0x00020000};
+    };
+    const intx4 from_w = buffer_of_side(0), from_w2 = buffer_of_side(kTwo ? 1 : 0), from_x = buffer_of_side(2);
+    // a lane's row of the eight, and its chunk's place
+    const int w_at = (lane >> 3) * (int)pitch + ((lane & 7) ^ ((lane >> 3 & 3) | (wave >> 1 & 1) << 2)) * 16;
+    const int x_at = (lane >> 3) * (int)pitch + ((lane & 7) ^ (lane >> 3)) * 16;
+    auto fetch = [&](int i, int t) {
+        const int side = side_of(i * kTogether), first = i * kTogether + wave * 8, row = min(row_of(i * kTogether) + wave * 8, side == 2 ? x_last : w_last);
+        fetch16(side == 2 ? from_x : side == 1 ? from_w2 : from_w, lds0 + (uint32_t)((t & (NS - 1)) * S::kStage + first * 128), (uint32_t)(side == 2 ? x_at : w_at),
+                (uint32_t)(row * (int)pitch + min(t, pieces - 1) * 128));
     };
     // Scales of a group of four stages, four bytes for each row of LDS: in a register for three stages, then in LDS, where two groups have a place.
     // There a word is what a lane needs for four tiles: the matrix instruction selects its byte.
@@ -232,7 +223,9 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             for (int i = 0; i < pieces; ++i) words[k] |= (uint32_t)scales_at[k][i] << (8 * i);
         }
     }
-    for (int t = 0; t < NS; ++t) fetch_stage(t);
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int i = 0; i < S::kFetches; ++i) fetch(i, t);
     put_scales(0, 0);
     wait_fetches<0>();
     meet();
@@ -250,12 +243,22 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
 #pragma unroll
         for (int g = 0; g < S::kGroupsM; ++g) sb[g] = next_sb[g];
         if (STEP == 0 && LOOP) fetch_scales(t + 4);
-        auto multiply = [&](int ha, int part, int hb) {
+        // The fetches of the stage NS ahead are issued between the products behind the meeting, from number `done` on: together they would hold those up.
+        constexpr int kProducts = S::kHN * S::kTM, kEach = (S::kFetches + kProducts - 1) / kProducts;
+        auto fetch_behind = [&](int done) {
+#pragma unroll
+            for (int i = done * kEach; i < min((done + 1) * kEach, S::kFetches); ++i) {
+                fetch(i, t + NS);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto multiply = [&](int ha, int part, int hb, int done = -1000) {
 #pragma unroll
             for (int i = part * S::kPart; i < (part + 1) * S::kPart; ++i)
 #pragma unroll
                 for (int j = 0; j < S::kHM; ++j) {
                     const int n = ha * S::kHN + i, m = (S::kTM > 1 ? hb * S::kHM : 0) + j;
+                    if (done >= 0) fetch_behind(done + (i - part * S::kPart) * S::kHM + j);
                     multiply_tile(a[ha][i], b[hb][j], acc[n][m], sa[n / 4], sb[m / 4], n % 4, m % 4);
                 }
         };
@@ -284,7 +287,6 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             wait_fetches<(NS - 2) * S::kFetches>();
             if (STEP == 3) put_scales((t >> 2) + 1, 8 * max(0, min(t + 5 - pieces, 3)));
             meet();
-            fetch_stage(t + NS);
             go_on((NEXT - HERE) * S::kStage);
             read_scales(t + 1);
         };
@@ -296,6 +298,8 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             if (S::kTM > 1) widen_b(F ^ 1);
             multiply_half(0);
             next_stage();
+#pragma unroll
+            for (int i = 0; i < S::kFetches; ++i) fetch(i, t + NS);
             read_a(0, 0);
             read_a(0, 1);
             multiply_half(1);
@@ -311,16 +315,17 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             phase();
             next_stage();
             read_a(0, 0);
+            constexpr int kOf = S::kPart * S::kHM, kBefore = S::kTM > 1 ? 2 * kOf : 0;
             if (S::kTM > 1) {
-                multiply(1, 0, F ^ 1);
-                multiply(1, 1, F ^ 1);
+                multiply(1, 0, F ^ 1, 0);
+                multiply(1, 1, F ^ 1, kOf);
             }
             phase();
             read_b(F ^ 1);
-            multiply(1, 0, F);
+            multiply(1, 0, F, kBefore);
             phase();
             read_a(0, 1);
-            multiply(1, 1, F);
+            multiply(1, 1, F, kBefore + kOf);
             phase();
         }
     };
@@ -403,40 +408,62 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             }
             continue;
         }
+        auto sums = [&](int side, int j, float(&z)[16]) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = acc[(g + side) * 4 + i / 4][j][i % 4];
+        };
+        if constexpr (KIND == kGatedBackward) {
+            // all of dh is on its way before the first of it is waited for
+            Pack<D, 8> d[S::kTM][2];
+#pragma unroll
+            for (int j = 0; j < S::kTM; ++j) {
+                const long long m = min(m0 + wm * (16 * S::kTM) + j * 16 + r, A.s.rows - 1);
+                const D* at = static_cast<const D*>(A.t.dh) + m * A.s.dh_row + n;
+                d[j][0] = load8(at, left);
+                d[j][1] = load8(at + 8, left - 8);
+            }
+#pragma unroll
+            for (int j = 0; j < S::kTM; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int m = m0 + wm * (16 * S::kTM) + j * 16 + r;
+                if (m >= A.s.rows || left <= 0) continue;
+                float z[16], y[16];
+                sums(0, j, z);
+                sums(kTwo ? 1 : 0, j, y);
+                auto gradients = [&](auto act) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float gate = z[i], up = y[i];
+                        gated_gradients<decltype(act)::value>(gate, up, to_float(d[j][i / 8].v[i % 8]), z[i], y[i]);
+                    }
+                };
+                if (A.s.act == kActSilu) gradients(Const<kActSilu>{});
+                else if (A.s.act == kActRelu) gradients(Const<kActRelu>{});
+                else gradients(Const<kActNone>{});
+                store_results(A.t.out, m * A.s.out_row + n, A.s.out_type, left, z);
+                store_results(A.t.out2, m * A.s.out_row + n, A.s.out_type, left, y);
+            }
+            continue;
+        }
 #pragma unroll
         for (int j = 0; j < S::kTM; ++j) {
             __builtin_amdgcn_sched_barrier(0);
             const int m = m0 + wm * (16 * S::kTM) + j * 16 + r;
             if (m >= A.s.rows || left <= 0) continue;
-            float z[16], y[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = acc[g * 4 + i / 4][j][i % 4];
-            const long long at = m * A.s.out_row + n;
+            float z[16];
+            sums(0, j, z);
             if (KIND == kLinear) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) z[i] += add[i];
                 finish_sixteen(z, A.s.act);
-                store_results(A.t.out, at, A.s.out_type, left, z);
             } else {
+                float y[16];
+                sums(kTwo ? 1 : 0, j, y);
+                finish_sixteen(z, A.s.act);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] = acc[(g + (kTwo ? 1 : 0)) * 4 + i / 4][j][i % 4];
-                if (KIND == kGated) {
-                    finish_sixteen(z, A.s.act);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] *= y[i];
-                    store_results(A.t.out, at, A.s.out_type, left, z);
-                } else {
-                    float d[16];
-                    load_values(A.t.dh, m * A.s.dh_row + n, A.s.dh_type, left, d);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float gate = z[i], up = y[i];
-                        gated_gradients(gate, up, d[i], A.s.act, z[i], y[i]);
-                    }
-                    store_results(A.t.out, at, A.s.out_type, left, z);
-                    store_results(A.t.out2, at, A.s.out_type, left, y);
-                }
+                for (int i = 0; i < 16; ++i) z[i] *= y[i];
             }
+            store_results(A.t.out, m * A.s.out_row + n, A.s.out_type, left, z);
         }
     }
 }
@@ -487,8 +514,8 @@ hipError_t launch_shape(Args A, hipStream_t stream)
     A.by_tiles = make_fast_div((uint32_t)(A.tiles_n * A.tiles_m));
     A.by_band = make_fast_div((uint32_t)(kBand * A.tiles_n));
     A.by_last = make_fast_div((uint32_t)(A.tiles_m % kBand ? A.tiles_m % kBand : kBand));
-    auto launch = [&](auto sliced) {
-        constexpr auto kernel = product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS, decltype(sliced)::value != 0>;
+    auto launch = [&](auto sliced, auto of_dh) {
+        constexpr auto kernel = product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS, decltype(sliced)::value != 0, decltype(of_dh)>;
         static std::atomic<uint64_t> allowed{0};
         if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(kernel), allowed); e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)(A.tiles_n * A.tiles_m * A.slices)), dim3(S::kThreads), S::kLds, stream, A);
@@ -497,9 +524,12 @@ hipError_t launch_shape(Args A, hipStream_t stream)
     // (the largest tiles are taken where there are enough of them)
     if constexpr (BM < 256) {
         if (A.slices > 1)
-            if (const hipError_t e = launch(Const<1>{}); e != hipSuccess) return e;
+            if (const hipError_t e = launch(Const<1>{}, float{}); e != hipSuccess) return e;
     }
-    if (A.slices == 1) return launch(Const<0>{});
+    if (A.slices == 1) {
+        if constexpr (KIND == kGatedBackward) return with_type(A.s.dh_type, [&](auto of_dh) { return launch(Const<0>{}, of_dh); });
+        else return launch(Const<0>{}, float{});
+    }
     const int across = (A.s.out + 255) / 256;
     hipLaunchKernelGGL((product_join_kernel<KIND>), dim3((unsigned)((long long)across * A.s.rows)), dim3(256), 0, stream, A.s, A.t, A.partial, A.slices,
                        make_fast_div((uint32_t)across));

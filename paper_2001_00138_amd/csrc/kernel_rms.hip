@@ -8,6 +8,8 @@
 // Short rows share a wavefront or have one each; longer ones take up to sixteen wavefronts, which join their sums through LDS in their order, so
 // results repeat bit for bit.  Backward, a workgroup takes several rows, a stride apart, and keeps its sums of dgamma in registers; they are
 // joined, again in a fixed order, by a second launch.
+//
+// 16384 x 4096 bf16 (from memory): codes with the residual 93 us, 5.0 TB/s; backward 109 us with its joining, 4.9 TB/s.
 #include "fp8.hpp"
 #include "kernels.hpp"
 #include "operators.hpp"
@@ -36,7 +38,10 @@ Plan plan_of(const RmsShape& s, bool backward)
         return p;
     }
     p.rows = 1;
-    p.runs = runs <= 512 ? 1 : runs <= (backward ? 1024 * kHeldBackward : 1024) ? 2 : runs <= 1024 * kHeld && !backward ? kHeld : 0;
+    // One run a lane is fastest, but for workgroups whose wavefronts the four SIMDs do not share evenly (16384 x 5120 bf16 forward: 137 us with ten, 124 with two runs on
+    // five; 8192 columns 94 with one, 98 with two; 12288: 77 with two, 84 with four), and backward for so many that a CU has one workgroup (8192 x 8192: 133 and 120).
+    if (backward) p.runs = runs <= 768 ? 1 : runs <= 1024 * kHeldBackward ? kHeldBackward : 0;
+    else p.runs = runs <= 512 || (runs <= 1024 && (runs + 63) / 64 % 4 == 0) ? 1 : runs <= 2048 ? 2 : runs <= 1024 * kHeld ? kHeld : 0;
     p.lanes = p.runs ? ((runs + p.runs - 1) / p.runs + 63) / 64 * 64 : 1024;
     return p;
 }
@@ -153,110 +158,115 @@ __global__ __launch_bounds__(1024) void rms_backward_kernel(RmsShape s, int lane
                                                             T* dx, float* __restrict__ partial)
 {
     __shared__ float slots[2][16];
-    __shared__ float share[RUNS > 0 ? 256 * 8 : 1];
     const int group = rows > 1 ? (int)threadIdx.x / lanes : 0, l = (int)threadIdx.x - group * lanes;
-    constexpr int kRuns = RUNS > 0 ? RUNS : 1;
     const float per = 1.0f / (float)s.cols;
-    auto load = [&](long long r, int run, float(&d)[8], float(&v)[8]) {
-        const int left = s.cols - run * 8;
-        load8_floats(dy + r * s.y_row + run * 8, left, d);
-        load8_floats(x + r * s.x_row + run * 8, left, v);
-    };
-    // d: gamma dy
-    auto finish = [&](long long r, int run, const float(&d)[8], const float(&v)[8], float scale, float back) {
-        const int left = s.cols - run * 8;
-        if (left <= 0) return;
-        float o[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = scale * d[j] - back * v[j];
-        if (dsum) {
-            float add[8];
-            load8_floats(dsum + r * s.residual_row + run * 8, left, add);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] += add[j];
-        }
-        store8(dx + r * s.sum_row + run * 8, left, o);
-    };
-    float g[kRuns][8], sums[kRuns][8];
-#pragma unroll
-    for (int i = 0; i < kRuns; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sums[i][j] = 0.0f;
-    if constexpr (RUNS > 0)
-#pragma unroll
-        for (int i = 0; i < kRuns; ++i) load_gamma(gamma, l + i * lanes, s.cols, g[i]);
     int turn = 0;
-    for (long long r = (long long)blockIdx.x * rows + group; r < s.rows; r += row_step, turn ^= 1) {
-        const float scale = rstd[r];
-        float dot = 0.0f;
-        if constexpr (RUNS > 0) {
-            float d[kRuns][8], v[kRuns][8];
+    if constexpr (RUNS == 0) {
+        for (long long r = blockIdx.x; r < s.rows; r += row_step, turn ^= 1) {
+            const float scale = rstd[r];
+            float d[8], v[8], g[8], dot = 0.0f;
+            auto load = [&](int run) {
+                const int left = s.cols - run * 8;
+                load8_floats(dy + r * s.y_row + run * 8, left, d);
+                load8_floats(x + r * s.x_row + run * 8, left, v);
+                load_gamma(gamma, run, s.cols, g);
 #pragma unroll
-            for (int i = 0; i < kRuns; ++i) load(r, l + i * lanes, d[i], v[i]);
+                for (int j = 0; j < 8; ++j) d[j] *= g[j], v[j] *= scale;
+            };
+            for (int run = l; run * 8 < s.cols; run += lanes) {
+                load(run);
 #pragma unroll
-            for (int i = 0; i < kRuns; ++i)
+                for (int j = 0; j < 8; ++j) dot += d[j] * v[j];
+            }
+            const float back = scale * (row_sum(dot, lanes, slots[turn]) * per);
+            for (int run = l; run * 8 < s.cols; run += lanes) {
+                load(run);
+                const int left = s.cols - run * 8;
+                float add[8] = {};
+                if (dsum) load8_floats(dsum + r * s.residual_row + run * 8, left, add);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[j] = scale * d[j] - back * v[j] + add[j];
+                store8(dx + r * s.sum_row + run * 8, left, d);
+            }
+        }
+    } else {
+        __shared__ float share[256 * 8];
+        float g[RUNS][8], sums[RUNS][8];
+#pragma unroll
+        for (int i = 0; i < RUNS; ++i) {
+            load_gamma(gamma, l + i * lanes, s.cols, g[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[i][j] = 0.0f;
+        }
+        for (long long r = (long long)blockIdx.x * rows + group; r < s.rows; r += row_step, turn ^= 1) {
+            // all of the row is on its way before any of it is waited for (asking for the next one too takes registers that more workgroups use better)
+            Pack<Y, 8> of_dy[RUNS];
+            Pack<T, 8> of_x[RUNS], of_dsum[RUNS];
+            const float scale = rstd[r];
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i) {
+                const int run = l + i * lanes, left = s.cols - run * 8;
+                of_dy[i] = load8(dy + r * s.y_row + run * 8, left);
+                of_x[i] = load8(x + r * s.x_row + run * 8, left);
+                if (dsum) of_dsum[i] = load8(dsum + r * s.residual_row + run * 8, left);
+            }
+            float d[RUNS][8], dot = 0.0f;
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float xh = v[i][j] * scale;
-                    sums[i][j] += d[i][j] * xh;
-                    d[i][j] *= g[i][j];
+                    const float xh = to_float(of_x[i].v[j]) * scale, of_y = to_float(of_dy[i].v[j]);
+                    sums[i][j] += of_y * xh;
+                    d[i][j] = of_y * g[i][j];
                     dot += d[i][j] * xh;
-                    v[i][j] = xh;
                 }
             const float back = scale * (row_sum(dot, lanes, slots[turn]) * per);
 #pragma unroll
-            for (int i = 0; i < kRuns; ++i) finish(r, l + i * lanes, d[i], v[i], scale, back);
-        } else {
-            float d[8], v[8];
-            for (int run = l; run * 8 < s.cols; run += lanes) {
-                load(r, run, d, v);
-                load_gamma(gamma, run, s.cols, g[0]);
+            for (int i = 0; i < RUNS; ++i) {
+                const int run = l + i * lanes, left = s.cols - run * 8;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dot += d[j] * g[0][j] * (v[j] * scale);
-            }
-            const float back = scale * (row_sum(dot, lanes, slots[turn]) * per);
-            for (int run = l; run * 8 < s.cols; run += lanes) {
-                load(r, run, d, v);
-                load_gamma(gamma, run, s.cols, g[0]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] *= g[0][j], v[j] *= scale;
-                finish(r, run, d, v, scale, back);
+                for (int j = 0; j < 8; ++j) {
+                    d[i][j] = scale * d[i][j] - back * (to_float(of_x[i].v[j]) * scale);
+                    if (dsum) d[i][j] += to_float(of_dsum[i].v[j]);
+                }
+                if (left > 0) store8(dx + r * s.sum_row + run * 8, left, d[i]);
             }
         }
-    }
-    if (RUNS == 0 || !partial) return;
-    float* to = partial + (long long)blockIdx.x * s.cols;
-    if (rows == 1) {
+        if (!partial) return;
+        float* to = partial + (long long)blockIdx.x * s.cols;
+        if (rows == 1) {
 #pragma unroll
-        for (int i = 0; i < kRuns; ++i)
-            if ((l + i * lanes) * 8 < s.cols) store8(to + (l + i * lanes) * 8, s.cols - (l + i * lanes) * 8, sums[i]);
-        return;
-    }
-    // rows that share a workgroup: their sums in the order of the groups
+            for (int i = 0; i < RUNS; ++i)
+                if ((l + i * lanes) * 8 < s.cols) store8(to + (l + i * lanes) * 8, s.cols - (l + i * lanes) * 8, sums[i]);
+            return;
+        }
+        // rows that share a workgroup: their sums in the order of the groups
 #pragma unroll
-    for (int j = 0; j < 8; ++j) share[threadIdx.x * 8 + j] = sums[0][j];
-    __syncthreads();
-    for (int c = (int)threadIdx.x; c < s.cols; c += (int)blockDim.x) {
-        float v = 0.0f;
-        for (int k = 0; k < rows; ++k) v += share[(k * lanes) * 8 + c];
-        to[c] = v;
+        for (int j = 0; j < 8; ++j) share[threadIdx.x * 8 + j] = sums[0][j];
+        __syncthreads();
+        for (int c = (int)threadIdx.x; c < s.cols; c += (int)blockDim.x) {
+            float v = 0.0f;
+            for (int k = 0; k < rows; ++k) v += share[(k * lanes) * 8 + c];
+            to[c] = v;
+        }
     }
 }
 
-// dgamma[c] = the sum of partial[0 ... count)[c]: 64 columns a workgroup, its sixteen wavefronts each a sixteenth of the rows.
+// dgamma[c] = the sum of partial[0 ... count)[c]: 32 columns a workgroup, its 32 half wavefronts each a part of the rows, eight on their way at a time.
 __global__ __launch_bounds__(1024) void rms_join_kernel(int cols, int count, const float* __restrict__ partial, float* __restrict__ dgamma)
 {
-    __shared__ float sums[16][64];
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const long long c = (long long)blockIdx.x * 64 + lane;
-    const int per = (count + 15) / 16, first = wave * per, last = min(first + per, count);
+    __shared__ float sums[32][32];
+    const int lane = (int)threadIdx.x & 31, part = (int)threadIdx.x >> 5;
+    const long long c = (long long)blockIdx.x * 32 + lane;
+    const int per = (count + 31) / 32, first = part * per, last = min(first + per, count);
     float v = 0.0f;
     if (c < cols)
+#pragma unroll 8
         for (int k = first; k < last; ++k) v += partial[(long long)k * cols + c];
-    sums[wave][lane] = v;
+    sums[part][lane] = v;
     __syncthreads();
-    if (wave || c >= cols) return;
-    for (int k = 1; k < 16; ++k) v += sums[k][lane];
+    if (part || c >= cols) return;
+    for (int k = 1; k < 32; ++k) v += sums[k][lane];
     dgamma[c] = v;
 }
 
@@ -273,13 +283,17 @@ __global__ __launch_bounds__(256) void rms_gamma_kernel(RmsShape s, int slab_row
     partial[(long long)blockIdx.y * s.cols + c] = v;
 }
 
-constexpr int kBackwardGroups = 512;                     // most workgroups of the backward pass that keep sums of dgamma
+// Most wavefronts a CU of the backward pass, whose workgroups keep sums of dgamma: all of them run at once, and every CU has as many (16384 x 4096 bf16 with 16, 24 and
+// 32: 120, 109 and 133 us); at least two rows each.
+constexpr int kBackwardWaves = 24, kBackwardWaves2 = 16; // with one run a lane, with two
 constexpr int kSlabs = 64;
 // Rows of partial sums of dgamma.
 int partial_rows(const RmsShape& s)
 {
     const Plan p = plan_of(s, true);
-    return p.runs ? (int)std::min<long long>(kBackwardGroups, ceil_div(s.rows, p.rows)) : (int)std::min(kSlabs, s.rows);
+    if (!p.runs) return std::min(kSlabs, s.rows);
+    const int each = std::max(1, (p.runs == 1 ? kBackwardWaves : kBackwardWaves2) * 64 / (p.lanes * p.rows));
+    return (int)std::min<long long>(256 * each, ceil_div(s.rows, 2 * p.rows));
 }
 
 }  // namespace
@@ -349,7 +363,7 @@ hipError_t launch_rms_backward(const RmsShape& s, const void* dy, const void* ds
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (!dgamma) return hipSuccess;
-    hipLaunchKernelGGL(rms_join_kernel, dim3((unsigned)((s.cols + 63ll) / 64)), dim3(1024), 0, stream, s.cols, count, partial, dgamma);
+    hipLaunchKernelGGL(rms_join_kernel, dim3((unsigned)((s.cols + 31ll) / 32)), dim3(1024), 0, stream, s.cols, count, partial, dgamma);
     return hipGetLastError();
 }
 

@@ -121,7 +121,8 @@ def test_backward(torch, rows, cols, kind):
         assert (np.abs(doubles(out[:, :cols]) - dx) <= off + U[kind] * (np.abs(dx) + off) + TINY[kind]).all()
         assert bool((out[:, cols:] == 77).all())
         size = (np.abs(doubles(dy)) * xh).sum(axis=0)
-        # a workgroup's rows, those that share it, and the joining of up to 512 workgroups by sixteen wavefronts; 64 slabs where rows are not held
+        # a workgroup's rows (two or three here), those that share it, and the joining of up to 650 workgroups by 32 half wavefronts: fewer than 64; 64 slabs where rows are
+        # not held
         steps = max(rows // 512, rows // 64 if cols > 16384 else 0) + 16 + 32 + 16
         assert (np.abs(doubles(dg) - dgamma) <= (steps + 3) * u * size + 2.0 ** -149).all()
 

@@ -413,20 +413,9 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
             for (int i = 0; i < 16; ++i) z[i] = acc[(g + side) * 4 + i / 4][j][i % 4];
         };
         if constexpr (KIND == kGatedBackward) {
-            // all of dh is on its way before the first of it is waited for
-            Pack<D, 8> d[S::kTM][2];
-#pragma unroll
-            for (int j = 0; j < S::kTM; ++j) {
-                const long long m = min(m0 + wm * (16 * S::kTM) + j * 16 + r, A.s.rows - 1);
-                const D* at = static_cast<const D*>(A.t.dh) + m * A.s.dh_row + n;
-                d[j][0] = load8(at, left);
-                d[j][1] = load8(at + 8, left - 8);
-            }
-#pragma unroll
-            for (int j = 0; j < S::kTM; ++j) {
-                __builtin_amdgcn_sched_barrier(0);
+            auto one = [&](int j, const Pack<D, 8>& d0, const Pack<D, 8>& d1) {
                 const int m = m0 + wm * (16 * S::kTM) + j * 16 + r;
-                if (m >= A.s.rows || left <= 0) continue;
+                if (m >= A.s.rows || left <= 0) return;
                 float z[16], y[16];
                 sums(0, j, z);
                 sums(kTwo ? 1 : 0, j, y);
@@ -434,7 +423,7 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const float gate = z[i], up = y[i];
-                        gated_gradients<decltype(act)::value>(gate, up, to_float(d[j][i / 8].v[i % 8]), z[i], y[i]);
+                        gated_gradients<decltype(act)::value>(gate, up, to_float(i < 8 ? d0.v[i % 8] : d1.v[i % 8]), z[i], y[i]);
                     }
                 };
                 if (A.s.act == kActSilu) gradients(Const<kActSilu>{});
@@ -442,6 +431,30 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
                 else gradients(Const<kActNone>{});
                 store_results(A.t.out, m * A.s.out_row + n, A.s.out_type, left, z);
                 store_results(A.t.out2, m * A.s.out_row + n, A.s.out_type, left, y);
+            };
+            auto dh_at = [&](int j) {
+                const long long m = min(m0 + wm * (16 * S::kTM) + j * 16 + r, A.s.rows - 1);
+                return static_cast<const D*>(A.t.dh) + m * A.s.dh_row + n;
+            };
+            if (n0 + kOut <= A.s.out) {
+                // dh is on its way before it is waited for: all of it, or in 32 bits two tiles ahead
+                constexpr int kMost = sizeof(D) == 4 ? 2 : 4, kDeep = S::kTM < kMost ? S::kTM : kMost;
+                Pack<D, 8> d[S::kTM][2];
+                auto ask = [&](int j) { d[j][0] = load_pack<D, 8>(dh_at(j)), d[j][1] = load_pack<D, 8>(dh_at(j) + 8); };
+#pragma unroll
+                for (int j = 0; j < kDeep; ++j) ask(j);
+#pragma unroll
+                for (int j = 0; j < S::kTM; ++j) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    one(j, d[j][0], d[j][1]);
+                    if (j + kDeep < S::kTM) ask(j + kDeep);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < S::kTM; ++j) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    one(j, load8(dh_at(j), left), load8(dh_at(j) + 8, left - 8));
+                }
             }
             continue;
         }

@@ -10,9 +10,6 @@
 // From memory: 1 x 12288 -> 4096 12.7 us, 4.0 TB/s of weights; gated 1 x 4096 -> 12288 21.9 us, 4.6 TB/s.
 #include "fp8_products.hpp"
 
-#ifdef FP8_TUNE
-extern "C" int patdnn_tune_fp8[4];
-#endif
 namespace patdnn {
 
 namespace {
@@ -103,9 +100,6 @@ hipError_t launch_rows(const ProductShape& s, const ProductTensors& t, hipStream
 // and 10.4; results in fp32 16.3 and 16.7).
 bool by_rows(const ProductShape& s)
 {
-#ifdef FP8_TUNE
-    if (patdnn_tune_fp8[3]) return patdnn_tune_fp8[3] == 1;
-#endif
     if (!product_tiles_fit(s)) return true;
     const long long weights = (long long)s.in * s.out * (s.kind == kLinear ? 1 : 2);
     return s.rows <= 8 || (s.rows <= kRows && (s.out_type == kF32 || weights < 48ll << 20));

@@ -298,11 +298,12 @@ int partial_rows(const RmsShape& s)
 
 }  // namespace
 
+// A grid has fewer than 2^32 threads: a workgroup for a row, or for several; backward, 64 threads for a column that is summed in slabs.
+constexpr int kMostBackwardColumns = (1 << 26) - 1024;
 bool rms_fits(const RmsShape& s, bool backward)
 {
-    if (s.cols > INT32_MAX - 8 * 1024 - 128) return false;
+    if (s.cols > (backward ? kMostBackwardColumns : INT32_MAX - 8 * 1024 - 128)) return false;
     const Plan p = plan_of(s, backward);
-    // a grid has fewer than 2^32 threads
     return backward || ceil_div(s.rows, p.rows) <= kMostBlocks * 256 / std::max(256, p.lanes);
 }
 

@@ -71,6 +71,13 @@ def test_rms_norm():
     _refused(B.PATDNN_EUNSUPPORTED, "large", f, _rms(cols=2 ** 31 - 1, x_row=0, sum_row=2 ** 31, y_row=2 ** 31), *good_f[1:])
     _refused(B.PATDNN_EUNSUPPORTED, "large", f, _rms(rows=2 ** 31 - 1, cols=1000, sum_row=1000, y_row=1000), *good_f[1:])
     _refused(B.PATDNN_EUNSUPPORTED, "large", f, _rms(x_row=1 << 60), *good_f[1:])
+    # backward: 64 threads for a column of a long row, in one grid
+    wide = dict(rows=1, x_row=0, residual_row=0, sum_row=1 << 30, y_row=0)
+    assert room(_rms(cols=2 ** 26 - 1024, **wide)) == 2 ** 26 - 1024 and room(_rms(cols=2 ** 26 - 1023, **wide)) == 0
+    _refused(B.PATDNN_EUNSUPPORTED, "large", b, _rms(cols=2 ** 26 - 1023, **wide), *good_b[1:])
+    _refused(B.PATDNN_EINVAL, "NULL", b, _rms(cols=2 ** 26 - 1024, **wide), None, *good_b[2:])
+    _refused(B.PATDNN_EINVAL, "NULL", f, _rms(cols=2 ** 31 - 8321, **{**wide, "sum_row": 1 << 31}), None, *good_f[2:])
+    _refused(B.PATDNN_EUNSUPPORTED, "large", f, _rms(cols=2 ** 31 - 8320, **{**wide, "sum_row": 1 << 31}), *good_f[1:])
     assert f(_rms(rows=0), None, None, None, None, None, None, None, None) == B.PATDNN_OK
     assert b(_rms(rows=0), None, None, None, None, None, None, None, None, 0, None) == B.PATDNN_OK
 

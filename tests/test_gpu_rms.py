@@ -62,7 +62,7 @@ def check_codes(codes, scales, y, off):
 
 
 SIZES = [(1, 1), (3, 5), (20, 64), (17, 128), (9, 130), (5, 256), (2, 300), (7, 511), (6, 513), (3, 1000), (2, 4096), (3, 4100), (2, 5120), (1, 8192), (2, 8200),
-         (2, 16384), (1, 20000), (1, 33000), (300, 40)]
+         (2, 16384), (1, 20000), (1, 33000), (1, 1 << 20), (300, 40)]
 
 
 @pytest.mark.parametrize("kind", KINDS)

@@ -561,7 +561,7 @@ Plan plan_of(const ProductShape& s)
 {
     const bool exact = s.out_type == kF32;
     const int pieces = (int)fp8_pieces(s.in);
-    // The largest tiles that three of four CUs get one of (256 x 4096 -> 12288, 192 tiles of 128^2: 26.5 us, 32 with 64^2; 512 x 4096 -> 4096, 128 of them: 25.9
+    // The largest tiles that three of four CUs get one of (256 x 4096 -> 12288, 192 tiles of 128^2: 23.5 us, 32 with 64^2; 512 x 4096 -> 4096, 128 of them: 25.9
     // and 19.5; gated 512 x 4096 -> 12288, 192 of 256 rows: 75 and 83).  Results in fp32 stop at 128 rows, which the gated pair's reach with fewer where k is
     // long enough to be cut (256 x 12288 -> 4096, 64 tiles: 65 us, 76 with 64 rows; backward 777 x 1500 -> 2100, 119 tiles: 35 us, 25 with 64 rows).
     constexpr long long kEnough = 192;
@@ -609,9 +609,12 @@ hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, 
     const bool exact = s.out_type == kF32;
     if (s.kind == kLinear) {
         if (exact) return p.rows == 128 ? launch_shape<kLinear, true, 128, 128, 2, 2, 2>(A, stream) : launch_shape<kLinear, true, 64, 64, 1, 4, 2>(A, stream);
-        return p.rows == 256   ? launch_shape<kLinear, false, 256, 256, 2, 4, 2>(A, stream)
-               : p.rows == 128 ? launch_shape<kLinear, false, 128, 128, 2, 2, 2>(A, stream)
-                               : launch_shape<kLinear, false, 64, 64, 1, 4, 4>(A, stream);
+        if (p.rows == 256) return launch_shape<kLinear, false, 256, 256, 2, 4, 2>(A, stream);
+        if (p.rows == 64) return launch_shape<kLinear, false, 64, 64, 1, 4, 4>(A, stream);
+        // A workgroup that has its CU to itself takes four stages; two on a CU cover each other's waits, and the LDS has room for them with two stages only
+        // (us with two and four: 1024 x 12288 -> 4096, 256 tiles, 77.7 and 61.6; 2048 x 4096 -> 4096, 512 of them, 37.8 and 43.1; fp32's products are long enough for two:
+        // 99.8 and 97.4, 67.5 and 78.1).
+        return tiles_of(s, 128, 128) <= 256 ? launch_shape<kLinear, false, 128, 128, 2, 2, 4>(A, stream) : launch_shape<kLinear, false, 128, 128, 2, 2, 2>(A, stream);
     }
     auto run = [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;

@@ -90,8 +90,9 @@ struct Tile {
 };
 
 // SLICED: sums of a slice of k go to A.partial.  D: dh's type.  (What is decided here and not in the kernel is what would cost it registers.)
-template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS, bool SLICED, class D>
-__global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
+// WAVES: of a SIMD, for which the compiler has to leave registers.
+template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS, int WAVES, bool SLICED, class D>
+__global__ __launch_bounds__(64 * WN * WM, WAVES) void product_tiles_kernel(Args A)
 {
     using S = Tile<BN, BM, WN, WM, NS>;
     constexpr bool kTwo = KIND != kLinear;
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Args A)
     // The wavefronts fetch eight rows each, of one side, and so on.  What lies past a side's end the buffer's own check keeps from being read (it compares a lane's part of the
     // offset with what the scalar part leaves, which is never past the last row); what stands in LDS there reaches only results that are dropped.
     constexpr int kTogether = 8 * S::kWaves;
-    static_assert(BN % kTogether == 0 && BM % kTogether == 0 && (!kTwo || kTogether == 64), "rows that are fetched together are of one side");
+    static_assert(BN % kTogether == 0 && BM % kTogether == 0 && (!kTwo || 64 % kTogether == 0), "rows that are fetched together are of one side");
     auto buffer_of_side = [&](int side) {
         const uint64_t p = (uint64_t)((side == 2 ? A.t.x + m0 * pitch : (side == 1 ? A.t.w2 : A.t.w) + n0 * pitch) + first_piece * 128);
         const long long bytes = ((long long)(side == 2 ? x_last : w_last) + 1) * pitch - first_piece * 128;
@@ -520,7 +521,8 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductShape s, Produ
     }
 }
 
-template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS>
+// CUT: whether a plan cuts such tiles along k.
+template <int KIND, bool EXACT, int BN, int BM, int WN, int WM, int NS, bool CUT, int WAVES = 1>
 hipError_t launch_shape(Args A, hipStream_t stream)
 {
     using S = Tile<BN, BM, WN, WM, NS>;
@@ -531,7 +533,7 @@ hipError_t launch_shape(Args A, hipStream_t stream)
     A.by_band = make_fast_div((uint32_t)(kBand * A.tiles_n));
     A.by_last = make_fast_div((uint32_t)(A.tiles_m % kBand ? A.tiles_m % kBand : kBand));
     auto launch = [&](auto sliced, auto of_dh) {
-        constexpr auto kernel = product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS, decltype(sliced)::value != 0, decltype(of_dh)>;
+        constexpr auto kernel = product_tiles_kernel<KIND, EXACT, BN, BM, WN, WM, NS, WAVES, decltype(sliced)::value != 0, decltype(of_dh)>;
         static std::atomic<uint64_t> allowed{0};
         if (const hipError_t e = allow_big_lds(reinterpret_cast<const void*>(kernel), allowed); e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)(A.tiles_n * A.tiles_m * A.slices)), dim3(S::kThreads), S::kLds, stream, A);
@@ -541,8 +543,7 @@ hipError_t launch_shape(Args A, hipStream_t stream)
         if constexpr (KIND == kGatedBackward) return with_type(A.s.dh_type, [&](auto of_dh) { return launch(Const<0>{}, of_dh); });
         else return launch(Const<0>{}, float{});
     }
-    // (the plan gives the largest tiles no slices)
-    if constexpr (BM == 256) return hipErrorInvalidValue;
+    if constexpr (!CUT) return hipErrorInvalidValue;
     else if (const hipError_t e = launch(Const<1>{}, float{}); e != hipSuccess) return e;
     const int across = (A.s.out + 255) / 256;
     hipLaunchKernelGGL((product_join_kernel<KIND>), dim3((unsigned)((long long)across * A.s.rows)), dim3(256), 0, stream, A.s, A.t, A.partial, A.slices,
@@ -562,14 +563,16 @@ Plan plan_of(const ProductShape& s)
     const bool exact = s.out_type == kF32;
     const int pieces = (int)fp8_pieces(s.in);
     // The largest tiles that three of four CUs get one of (256 x 4096 -> 12288, 192 tiles of 128^2: 23.5 us, 32 with 64^2; 512 x 4096 -> 4096, 128 of them: 25.9
-    // and 19.5; gated 512 x 4096 -> 12288, 192 of 256 rows: 75 and 83).  Results in fp32 stop at 128 rows, which the gated pair's reach with fewer where k is
-    // long enough to be cut (256 x 12288 -> 4096, 64 tiles: 65 us, 76 with 64 rows; backward 777 x 1500 -> 2100, 119 tiles: 35 us, 25 with 64 rows).
+    // and 19.5; gated 512 x 4096 -> 12288, 192 of 256 rows: 75 and 83).  Results in fp32 stop at 128 rows.  The gated pair's
+    // next are of 64 outputs, or 128 for the scale that they share (1003 x 2000 -> 3000, 192 tiles of 128 rows: 18 us, 30 with 64 rows), by 128 rows also with fewer
+    // tiles where k is long enough to be cut (600 x 12288 -> 1000, 80 tiles: 46 us, 69 by 64 rows uncut; 500 x 700 -> 2000, 128 of them: 11 and 9).
     constexpr long long kEnough = 192;
     Plan p{};
     if (s.kind == kLinear)
         p = !exact && tiles_of(s, 256, 256) >= kEnough ? Plan{256, 256} : tiles_of(s, 128, 128) >= kEnough ? Plan{128, 128} : Plan{64, 64};
-    else if (exact) p = tiles_of(s, 128, 128) >= (pieces >= 64 ? 64 : kEnough) ? Plan{128, 128} : Plan{128, 64};
-    else p = tiles_of(s, 128, 256) >= kEnough ? Plan{128, 256} : Plan{128, 64};
+    else if (!exact && tiles_of(s, 128, 256) >= kEnough) p = Plan{128, 256};
+    else if (s.out_type == kFp8) p = Plan{128, tiles_of(s, 128, 128) >= kEnough ? 128 : 64};
+    else p = Plan{64, tiles_of(s, 64, 128) >= (pieces >= 64 ? 64 : kEnough) ? 128 : 64};
     // Fewer tiles than CUs are cut along k, into slices of eight stages and more (four in fp32, whose take longer): adding them up is a launch of its own, whose
     // bytes cost what it saves where there are many rows (us in 1, 2, 4 and 8 slices: 32 x 4096 -> 4096 14.8, 12.3, 11.0, 12.5; 128 x 4096 -> 4096 15.1, 14.9, 17.0,
     // 22.7; 64 x 12288 -> 4096 36, 23, 17.7, 17.7; gated 256 x 12288 -> 4096 77, 54, 62, 89).  Linear layers' long slices of the smallest tiles pay up to twice as many
@@ -608,19 +611,30 @@ hipError_t launch_product_tiles(const ProductShape& s, const ProductTensors& t, 
     A.slice_pieces = p.slice_pieces;
     const bool exact = s.out_type == kF32;
     if (s.kind == kLinear) {
-        if (exact) return p.rows == 128 ? launch_shape<kLinear, true, 128, 128, 2, 2, 2>(A, stream) : launch_shape<kLinear, true, 64, 64, 1, 4, 2>(A, stream);
-        if (p.rows == 256) return launch_shape<kLinear, false, 256, 256, 2, 4, 2>(A, stream);
-        if (p.rows == 64) return launch_shape<kLinear, false, 64, 64, 1, 4, 4>(A, stream);
+        if (exact) return p.rows == 128 ? launch_shape<kLinear, true, 128, 128, 2, 2, 2, false, 2>(A, stream) : launch_shape<kLinear, true, 64, 64, 1, 4, 2, true>(A, stream);
+        if (p.rows == 256) return launch_shape<kLinear, false, 256, 256, 2, 4, 2, false>(A, stream);
+        if (p.rows == 64) return launch_shape<kLinear, false, 64, 64, 1, 4, 4, true>(A, stream);
         // A workgroup that has its CU to itself takes four stages; two on a CU cover each other's waits, and the LDS has room for them with two stages only
         // (us with two and four: 1024 x 12288 -> 4096, 256 tiles, 77.7 and 61.6; 2048 x 4096 -> 4096, 512 of them, 37.8 and 43.1; fp32's products are long enough for two:
         // 99.8 and 97.4, 67.5 and 78.1).
-        return tiles_of(s, 128, 128) <= 256 ? launch_shape<kLinear, false, 128, 128, 2, 2, 4>(A, stream) : launch_shape<kLinear, false, 128, 128, 2, 2, 2>(A, stream);
+        return tiles_of(s, 128, 128) <= 256 ? launch_shape<kLinear, false, 128, 128, 2, 2, 4, false>(A, stream) : launch_shape<kLinear, false, 128, 128, 2, 2, 2, false>(A, stream);
     }
     auto run = [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
-        if constexpr (KIND != kGatedCodes)
-            if (exact) return p.rows == 128 ? launch_shape<KIND, true, 256, 128, 2, 4, 2>(A, stream) : launch_shape<KIND, true, 256, 64, 2, 4, 2>(A, stream);
-        return p.rows == 256 ? launch_shape<KIND, false, 256, 256, 2, 4, 2>(A, stream) : launch_shape<KIND, false, 256, 64, 2, 4, 2>(A, stream);
+        if (p.rows == 256) return launch_shape<KIND, false, 256, 256, 2, 4, 2, false>(A, stream);
+        if constexpr (KIND == kGatedCodes) {
+            return p.rows == 128 ? launch_shape<KIND, false, 256, 128, 2, 4, 2, false>(A, stream) : launch_shape<KIND, false, 256, 64, 2, 4, 2, true>(A, stream);
+        } else if (const bool alone = tiles_of(s, 64, 128) * p.slices <= 256; exact) {
+            if (p.rows == 64) return launch_shape<KIND, true, 128, 64, 1, 4, 2, true>(A, stream);
+            // (registers for two workgroups on a CU where there are as many, 4096 x 4096 -> 8192 backward: 521 us, 576 in tiles of 256 x 128; else as many as the
+            // compiler likes: 777 x 1500 -> 2100 23.0, 25.1 with those for two)
+            return alone ? launch_shape<KIND, true, 128, 128, 1, 4, 2, true>(A, stream) : launch_shape<KIND, true, 128, 128, 1, 4, 2, false, 2>(A, stream);
+        } else {
+            if (p.rows == 64) return launch_shape<KIND, false, 128, 64, 1, 4, 2, true>(A, stream);
+            // (four stages as above, where k is long enough to make up for their start: 512 x 4096 -> 4096, 256 tiles, 26.2 us with two and 21.5 with four;
+            // 777 x 1500 -> 2100 11.4 and 11.8; 1003 x 2000 -> 3000, 376 tiles, 19.4 and 24.4)
+            return alone && A.pieces >= 16 ? launch_shape<KIND, false, 128, 128, 1, 4, 4, true>(A, stream) : launch_shape<KIND, false, 128, 128, 1, 4, 2, false>(A, stream);
+        }
     };
     return s.kind == kGatedBackward ? run(Const<kGatedBackward>{}) : s.out_type == kFp8 ? run(Const<kGatedCodes>{}) : run(Const<kGated>{});
 }

@@ -205,10 +205,12 @@ def test_graph_and_no_rows(torch):
 
 
 # (sizes that take each tile shape, with rows and outputs that end inside a tile, and k of one to nine stages; and slices of k, of eight pieces and more, the last of
-# three; and long sums in as few of the larger tiles as take them; and one to six stages where a CU has one tile of 128 by 128)
+# three; and long sums in as few of the larger tiles as take them; and one to six stages where a CU has one tile of 128 by 128, of
+# linear layers and of the gated pair; and slices of its tiles of 64 outputs by 128 rows)
 LARGE = [(4090, 300, 4100), (2100, 520, 2000), (520, 1100, 700), (8200, 128, 2050), (300, 1030, 33000), (40, 5000, 300), (70, 4100, 1000), (20, 7200, 130),
          (3500, 6200, 3600), (1500, 6200, 2000), (300, 8200, 2000), (1500, 100, 2000), (2000, 250, 1590),
-         (1030, 380, 3500), (2040, 500, 2040), (1900, 640, 1700), (1900, 700, 1700)]
+         (1030, 380, 3500), (2040, 500, 2040), (1900, 640, 1700), (1900, 700, 1700), (1800, 100, 1000), (1000, 370, 2000),
+         (1000, 2100, 2000), (900, 8200, 700), (1400, 9000, 350)]
 
 
 def whole(torch, rows, k, squares, seed):

@@ -8,9 +8,9 @@
 // LDS holds 16-byte chunks, eight a row; a chunk of a row stands at its place xor a number that depends on the row, chosen so that the eight lanes
 // that are served in one cycle find theirs in different banks.  The weights' rows of a wavefront are dealt to the instruction's rows so that a lane's
 // results for four tiles are sixteen neighbouring outputs.  For the gated pair, each 64 rows of the first projection's are followed by the same 64 of the second's,
-// so that one lane has both sums of an output, and a workgroup all 128 outputs that share a scale.
+// so that one lane has both sums of an output, and a workgroup whose result is codes all 128 outputs that share a scale.
 //
-// 8192 x 8192 values, 8192 outputs, bf16: 407 us, 2.70 PFLOP/s (335 without the fetches); the matrix cores are busy 64 % of the cycles, at 1.69 GHz of 2.4.  fp32: 890 us.
+// 8192 x 8192 values, 8192 outputs, bf16: 407 us, 2.70 PFLOP/s (335 without the fetches); the matrix cores are busy 64 % of the cycles, at 1.69 GHz of 2.4.  fp32: 880 us.
 // Gated, 8192 x 4096 -> 12288: codes 650 us, bf16 640; its gradients 785.
 #include "fp8_products.hpp"
 

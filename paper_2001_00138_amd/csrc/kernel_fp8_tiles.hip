@@ -563,7 +563,7 @@ Plan plan_of(const ProductShape& s)
     const bool exact = s.out_type == kF32;
     const int pieces = (int)fp8_pieces(s.in);
     // The largest tiles that three of four CUs get one of (256 x 4096 -> 12288, 192 tiles of 128^2: 23.5 us, 32 with 64^2; 512 x 4096 -> 4096, 128 of them: 25.9
-    // and 19.5; gated 512 x 4096 -> 12288, 192 of 256 rows: 75 and 83).  Results in fp32 stop at 128 rows.  The gated pair's
+    // and 19.5; gated 512 x 4096 -> 12288, 192 of 256 rows: 54 and 63).  Results in fp32 stop at 128 rows.  The gated pair's
     // next are of 64 outputs, or 128 for the scale that they share (1003 x 2000 -> 3000, 192 tiles of 128 rows: 18 us, 30 with 64 rows), by 128 rows also with fewer
     // tiles where k is long enough to be cut (600 x 12288 -> 1000, 80 tiles: 46 us, 69 by 64 rows uncut; 500 x 700 -> 2000, 128 of them: 11 and 9).
     constexpr long long kEnough = 192;
@@ -575,7 +575,7 @@ Plan plan_of(const ProductShape& s)
     else p = Plan{64, tiles_of(s, 64, 128) >= (pieces >= 64 ? 64 : kEnough) ? 128 : 64};
     // Fewer tiles than CUs are cut along k, into slices of eight stages and more (four in fp32, whose take longer): adding them up is a launch of its own, whose
     // bytes cost what it saves where there are many rows (us in 1, 2, 4 and 8 slices: 32 x 4096 -> 4096 14.8, 12.3, 11.0, 12.5; 128 x 4096 -> 4096 15.1, 14.9, 17.0,
-    // 22.7; 64 x 12288 -> 4096 36, 23, 17.7, 17.7; gated 256 x 12288 -> 4096 77, 54, 62, 89).  Linear layers' long slices of the smallest tiles pay up to twice as many
+    // 22.7; 64 x 12288 -> 4096 36, 23, 17.7, 17.7; gated codes 256 x 12288 -> 4096 77, 54, 62, 89).  Linear layers' long slices of the smallest tiles pay up to twice as many
     // (256 x 12288 -> 4096 37, 33, 37).  The largest tiles are whole.
     const long long tiles = tiles_of(s, p.outputs, p.rows);
     long long slices = p.rows == 256 ? 1 : std::max<long long>(1, std::min<long long>(pieces / (exact ? 4 : 8), 256 / tiles));

@@ -90,7 +90,7 @@ __global__ __launch_bounds__(1024) void rms_kernel(RmsShape s, int lanes, int ro
                                                    const float* __restrict__ gamma, T* sum, void* __restrict__ y, uint8_t* __restrict__ scales,
                                                    float* __restrict__ rstd)
 {
-    __shared__ float slots[16];
+    __shared__ float slots[2][16];
     const int group = rows > 1 ? (int)threadIdx.x / lanes : 0, l = (int)threadIdx.x - group * lanes;
     const long long r = (long long)blockIdx.x * rows + group;
     if (r >= s.rows) return;                                             // (only where rows share a workgroup, which has no barrier)
@@ -117,9 +117,17 @@ __global__ __launch_bounds__(1024) void rms_kernel(RmsShape s, int lanes, int ro
         for (int j = 0; j < 8; ++j) v[j] = v[j] * scale * g[j];
         put<Y>(s, pieces, row, run, v, y, scales);
     };
-    float total = 0.0f;
+    // 1 / sqrt(mean + eps) from this lane's sum of squares; again(factor): that of the values times a power of two.  A sum may pass fp32's range where the mean does not: it is made again in
+    // units of 2^16 (columns are fewer than 2^32), from which a mean beyond the range is infinite and its root 0.  (All lanes of a row have the same sum.)
+    auto root = [&](float total, auto again) {
+        float mean = row_sum(total, lanes, slots[0]) / (float)s.cols;
+        if (mean == __builtin_inff()) mean = row_sum(again(0x1p-16f), lanes, slots[1]) / (float)s.cols * 0x1p32f;
+        const float scale = 1.0f / sqrtf(mean + s.eps);
+        if (rstd && l == 0) rstd[r] = scale;
+        return scale;
+    };
     if constexpr (RUNS > 0) {
-        float v[RUNS][8];
+        float v[RUNS][8], total = 0.0f;
 #pragma unroll
         for (int i = 0; i < RUNS; ++i) load(l + i * lanes, v[i]);
 #pragma unroll
@@ -128,21 +136,30 @@ __global__ __launch_bounds__(1024) void rms_kernel(RmsShape s, int lanes, int ro
 #pragma unroll
             for (int j = 0; j < 8; ++j) total += v[i][j] * v[i][j];
         }
-        const float scale = 1.0f / sqrtf(row_sum(total, lanes, slots) / (float)s.cols + s.eps);
-        if (rstd && l == 0) rstd[r] = scale;
+        const float scale = root(total, [&](float factor) {
+            float sum2 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum2 += (v[i][j] * factor) * (v[i][j] * factor);
+            return sum2;
+        });
 #pragma unroll
         for (int i = 0; i < RUNS; ++i) finish(l + i * lanes, v[i], scale);
     } else {
         // sum may be residual itself, so it is written after the second reading
         const int runs = pieces * 16;
         float v[8];
-        for (int run = l; run < runs; run += lanes) {
-            load(run, v);
+        auto squares = [&](float factor) {
+            float sum2 = 0.0f;
+            for (int run = l; run < runs; run += lanes) {
+                load(run, v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) total += v[j] * v[j];
-        }
-        const float scale = 1.0f / sqrtf(row_sum(total, lanes, slots) / (float)s.cols + s.eps);
-        if (rstd && l == 0) rstd[r] = scale;
+                for (int j = 0; j < 8; ++j) sum2 += (v[j] * factor) * (v[j] * factor);
+            }
+            return sum2;
+        };
+        const float scale = root(squares(1.0f), squares);
         for (int run = l; run < runs; run += lanes) {
             load(run, v);
             keep(run, v);

@@ -602,8 +602,8 @@ patdnn_status_t patdnn_fp8_dequantize(const uint8_t* codes, const uint8_t* scale
  *   dy                 `y_type` (no codes);  dsum, s, dx  `type`; dsum NULL: none.  dx may be dsum itself.
  *   dgamma             fp32 [cols] or NULL; written, not added to (zeros for rows == 0)
  *   workspace          patdnn_rms_norm_workspace_floats floats for the backward call with dgamma, contents undefined before and after
- * Strides in elements between rows, values of a row adjacent (inputs >= 0, outputs >= cols).  Squares are added in fp32: a row with a mean square beyond its range
- * has rstd 0.  Results repeat bit for bit.  rows == 0 is a no-op but for dgamma.  PATDNN_EUNSUPPORTED beyond 2^31 - 8321 columns (backward 2^26 - 1024)
+ * Strides in elements between rows, values of a row adjacent (inputs >= 0, outputs >= cols).  Squares are added in fp32, in units that hold them: only a row with a
+ * mean square beyond its range has rstd 0, and only one whose rstd is (a row of zeros and eps 0) has infinity.  Results repeat bit for bit.  rows == 0 is a no-op but for dgamma.  PATDNN_EUNSUPPORTED beyond 2^31 - 8321 columns (backward 2^26 - 1024)
  * and 2^24 workgroups (of a row, or of several short ones).
  */
 typedef struct {

@@ -118,11 +118,18 @@ __global__ __launch_bounds__(1024) void rms_kernel(RmsShape s, int lanes, int ro
         put<Y>(s, pieces, row, run, v, y, scales);
     };
     // 1 / sqrt(mean + eps) from this lane's sum of squares; again(factor): that of the values times a power of two.  A sum may pass fp32's range where the mean does not: it is made again in
-    // units of 2^16 (columns are fewer than 2^32), from which a mean beyond the range is infinite and its root 0.  (All lanes of a row have the same sum.)
+    // units of 2^16 (columns are fewer than 2^32), from which a mean beyond the range is infinite and its root 0.  Squares below the range are lost: they count where neither the mean nor eps is
+    // 2^-100, and are made again in units of 2^-80 (no value is 2^-34 then, whose square times 2^31 columns stays in range).  (All lanes of a row have the same sum.)
     auto root = [&](float total, auto again) {
         float mean = row_sum(total, lanes, slots[0]) / (float)s.cols;
-        if (mean == __builtin_inff()) mean = row_sum(again(0x1p-16f), lanes, slots[1]) / (float)s.cols * 0x1p32f;
-        const float scale = 1.0f / sqrtf(mean + s.eps);
+        const bool over = mean == __builtin_inff(), under = mean < 0x1p-100f && s.eps < 0x1p-100f;
+        float scale;
+        if (over || under) {
+            mean = row_sum(again(over ? 0x1p-16f : 0x1p80f), lanes, slots[1]) / (float)s.cols;
+            scale = over ? 1.0f / sqrtf(mean * 0x1p32f + s.eps) : 0x1p80f / sqrtf(mean + s.eps * 0x1p80f * 0x1p80f);
+        } else {
+            scale = 1.0f / sqrtf(mean + s.eps);
+        }
         if (rstd && l == 0) rstd[r] = scale;
         return scale;
     };

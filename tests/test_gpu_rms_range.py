@@ -1,6 +1,6 @@
-"""Root-mean-square norm of rows whose squares pass fp32's range though their mean does not.
+"""Root-mean-square norm of rows whose squares pass fp32's range though their mean does not, and of rows whose squares fall below it though the root of their mean does not.
 
-Tolerances as in the tests of ordinary rows: powers of two that a row is scaled by have no rounding, and squares that they take below fp32's smallest are less than 2^-100 of the sum."""
+Tolerances as in the tests of ordinary rows: powers of two that a row is scaled by have no rounding, and squares that fall below fp32's smallest are less than 2^-40 of the sum."""
 
 import numpy as np
 import pytest
@@ -28,7 +28,7 @@ def check(torch, rows, kind, eps, normal):
     """rows [n][cols] in `kind`, with ordinary ones beside them, keep their results; `normal`: those that do."""
     x = stored(torch, rows, kind)
     gamma = np.linspace(-1.5, 1.5, rows.shape[1]).astype(np.float32)
-    y, s, rstd = ff.rms_norm(doubles(x), None, gamma, eps)
+    y, s, rstd = ff.rms_norm(doubles(x), None, gamma, float(np.float32(eps)))
     rel = (chain(rows.shape[1]) / 2 + 8) * u
     args = dict(eps=eps, residual=torch.zeros_like(x).cuda())
     for out in ("f32", "bf16"):
@@ -54,3 +54,17 @@ def test_sum_of_squares_beyond_the_range(torch, cols, kind):
     assert (np.square(rows[[0, 2, 5]]).sum(axis=1) > 2.0 ** 128).all()
     rstd = check(torch, rows, kind, 1e-6, [0, 1, 2, 4, 5])
     assert rstd[3] == 0
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", COLS)
+def test_squares_below_the_range(torch, cols, kind):
+    """Squares that fp32 cannot hold, without an eps that they vanish beside; a larger value among them, and eps, come first where they are there."""
+    rng = np.random.default_rng([cols, 1])
+    rows = rng.standard_normal((7, cols))
+    for i, size in ((0, 1e-19), (2, 1e-23), (3, 1e-30), (5, 3e-36)):
+        rows[i] *= size
+    rows[4] *= 1e-25
+    rows[4, cols // 2] = 1e-3
+    for eps in (0.0, 1e-42, 1e-31, 1e-6):
+        check(torch, rows, kind, eps, slice(None))

@@ -846,7 +846,7 @@ def _new_codes(out, scales, rows: int, pieces: int, like, stream, name="output")
     else:
         if tuple(out.shape) != (rows, pieces * 128):
             raise ValueError(f"{name} must be {(rows, pieces * 128)}")
-        op = _byte_codes(out, name)
+        op = _byte_codes(out, name) if pieces else _devptr(out)        # (of the transpose of no rows)
     if scales is None:
         scales = _new((rows, pieces), _modules["torch"].uint8, like, stream)
         return out, scales, op, scales.data_ptr()

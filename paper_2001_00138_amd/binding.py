@@ -945,7 +945,10 @@ def patdnn_rms_norm(x, gamma=None, out=None, *, residual=None, sum=None, eps=1e-
 
 def patdnn_rms_norm_backward(dy, sum, rstd, gamma=None, out=None, *, dsum=None, dgamma=None, workspace=None, stream=None):
     """Gradients of patdnn_rms_norm: (dx like sum, dgamma float32 [cols]) from dy (of any type), the forward call's sum and rstd.  ``dsum``: the gradient that
-    arrives along the residual stream, added to dx; ``out=dsum`` adds in place."""
+    arrives along the residual stream, added to dx; ``out=dsum`` adds in place.  ``dgamma=False``: None in its place, which saves the call its workspace and second launch."""
+    wanted = dgamma is not False
+    if not wanted:
+        dgamma = workspace = None
     device = _together(sum, dy, rstd, gamma, out, dsum, dgamma, workspace)
     torch = _modules["torch"]
     s_row = _rows(sum, "sum")
@@ -956,13 +959,16 @@ def patdnn_rms_norm_backward(dy, sum, rstd, gamma=None, out=None, *, dsum=None, 
         out = _new((rows, cols), sum.dtype, sum, stream)
     desc = RmsDesc(rows, cols, _type(sum.dtype), _type(dy.dtype), 0.0, s_row, 0 if dsum is None else _typed_rows(dsum, sum.shape, sum.dtype, "dsum"),
                    _typed_rows(out, sum.shape, sum.dtype, "output"), _rows(dy, "dy"))
-    dgamma, gp = _row_floats(dgamma, cols, "dgamma", sum, stream)
-    if workspace is None:
-        workspace = _new((lib().patdnn_rms_norm_workspace_floats(ctypes.byref(desc)),), torch.float32, sum, stream)
-    elif workspace.dtype != torch.float32:
-        raise ValueError("workspace must be a float32 tensor")
+    gp, wp, floats = None, None, 0
+    if wanted:
+        dgamma, gp = _row_floats(dgamma, cols, "dgamma", sum, stream)
+        if workspace is None:
+            workspace = _new((lib().patdnn_rms_norm_workspace_floats(ctypes.byref(desc)),), torch.float32, sum, stream)
+        elif workspace.dtype != torch.float32:
+            raise ValueError("workspace must be a float32 tensor")
+        wp, floats = _devptr(workspace), workspace.numel()
     _call(device, stream, lib().patdnn_rms_norm_backward, ctypes.byref(desc), dy.data_ptr(), None if dsum is None else dsum.data_ptr(), sum.data_ptr(),
-          _float_vector(rstd, rows, "rstd"), _float_vector(gamma, cols, "gamma"), out.data_ptr(), gp, _devptr(workspace), workspace.numel())
+          _float_vector(rstd, rows, "rstd"), _float_vector(gamma, cols, "gamma"), out.data_ptr(), gp, wp, floats)
     return out, dgamma
 
 

@@ -524,7 +524,7 @@ patdnn_status_t patdnn_group_norm_backward(const patdnn_norm_desc_t* desc, const
  * a value becomes the nearest code to value / 2^(b - 127), ties to the even code, magnitudes above 6 become 6.
  * A block that holds something not finite has b = 255 and zero codes; its values read back as NaN.
  *   x / out: `type`, `row` elements between rows (out: >= cols), values of a row adjacent.
- * PATDNN_EUNSUPPORTED beyond 2^24 workgroups of 2048 values (each of whole rows, or of part of one).
+ * PATDNN_EUNSUPPORTED beyond 2^24 - 1 workgroups of 2048 values (each of whole rows, or of part of one).
  * rows == 0 is a no-op.
  */
 patdnn_status_t patdnn_mxfp4_quantize(const void* x, int32_t type, int32_t rows, int32_t cols, int64_t row, uint8_t* codes,
@@ -541,7 +541,7 @@ patdnn_status_t patdnn_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sca
  *   bias         fp32 [out_features] or NULL
  *   workspace    patdnn_mxfp4_linear_workspace_bytes bytes, 16-byte aligned (may be NULL if that is 0), contents
  *                undefined before and after; calls that share one must not overlap in time
- * Results repeat bit for bit.  rows == 0 is a no-op.  PATDNN_EUNSUPPORTED beyond 2^26 outputs, 2^31 - 257 rows, and where a launch would have more
+ * Results repeat bit for bit.  rows == 0 is a no-op.  PATDNN_EUNSUPPORTED beyond 2^26 - 16 outputs, 2^31 - 257 rows, and where a launch would have more
  * than some 2^22 workgroups (of 256 x 256 outputs; up to 512 input features are bounded by rows and outputs only).
  */
 typedef struct {
@@ -578,7 +578,7 @@ patdnn_status_t patdnn_mxfp4_linear(const patdnn_linear_desc_t* desc, const void
  *   patdnn_fp8_quantize    x [rows][cols], `row` elements between rows (>= 0) -> its codes and scales; with `transposed` those of the
  *       transpose, [cols][ceil(rows / 128) * 128]: what a product that sums over x's rows reads
  *   patdnn_fp8_dequantize  the values [rows][cols] that codes and scales stand for, `row` elements between rows (>= cols)
- * rows == 0 is a no-op (with `transposed` too).  PATDNN_EUNSUPPORTED beyond 2^24 workgroups of 2048 values in a launch (of 128 x 128, where
+ * rows == 0 is a no-op (with `transposed` too).  PATDNN_EUNSUPPORTED beyond 2^24 - 1 workgroups of 2048 values in a launch (of 128 x 128, where
  * blocks are squares or the matrix is transposed).
  */
 #define PATDNN_FP8_ROWS    0
@@ -604,7 +604,8 @@ patdnn_status_t patdnn_fp8_dequantize(const uint8_t* codes, const uint8_t* scale
  *   workspace          patdnn_rms_norm_workspace_floats floats for the backward call with dgamma, contents undefined before and after
  * Strides in elements between rows, values of a row adjacent (inputs >= 0, outputs >= cols).  Squares are added in fp32, in units that hold them: only a row with a
  * mean square beyond its range has rstd 0, and only one whose rstd is (a row of zeros and eps 0) has infinity.  Results repeat bit for bit.  rows == 0 is a no-op but for dgamma.  PATDNN_EUNSUPPORTED beyond 2^31 - 8321 columns (backward 2^26 - 1024)
- * and 2^24 workgroups (of a row, or of several short ones).
+ * and, forward, beyond what a grid of fewer than 2^32 threads holds: 2^28 - 16 rows of up to 128 columns (16 threads a row), 2^22 - 1 rows of 8192 and more (1024 threads),
+ * in proportion between.
  */
 typedef struct {
     int32_t rows, cols;
@@ -639,8 +640,8 @@ patdnn_status_t patdnn_rms_norm_backward(const patdnn_rms_desc_t* desc, const vo
  *   dh            `dh_type`, `dh_row` elements between rows (read by the backward call only)
  *   workspace     the bytes that the call's own function names, 16-byte aligned (may be NULL if that is 0), contents undefined
  *                 before and after; calls that share one must not overlap in time
- * A block with scale 255 makes every sum that it is part of NaN.  Results repeat bit for bit.  rows == 0 is a no-op.  PATDNN_EUNSUPPORTED beyond 2^26 outputs, 2^31 - 257 rows,
- * and where a launch would have more than some 2^22 workgroups.
+ * A block with scale 255 makes every sum that it is part of NaN.  Results repeat bit for bit.  rows == 0 is a no-op.  PATDNN_EUNSUPPORTED beyond 2^26 - 16 outputs
+ * and beyond 2^22 - 1 tiles of 64 x 64 results (beyond 8388480 input features, of 16 x 16).
  */
 typedef struct {
     int32_t rows, in_features, out_features;

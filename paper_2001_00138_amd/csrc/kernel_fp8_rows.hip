@@ -95,14 +95,14 @@ hipError_t launch_rows(const ProductShape& s, const ProductTensors& t, hipStream
     return hipGetLastError();
 }
 
-// Whether the call is for this kernel and not for tiles: up to 16 rows, but from nine on tiles read x less often where there are many weights and the sums are the fp8
-// instruction's (16 rows, us here and in tiles: 12288 -> 4096 16.3 and 14.4, 4096 -> 12288 16.3 and 14.7, gated 24.5 and 22.8; 8 rows 13.1 and 14.2; 16 x 4096 -> 4096 7.8
-// and 10.4; results in fp32 16.3 and 16.7).
+// Whether the call is for this kernel and not for tiles: up to 16 rows, but linear layers on the fp8 instruction's sums from 1.25 * 2^30 products on, with nine rows or more: there tiles, which
+// read x less often, are faster (us here and in tiles, weights from memory: 16 rows 8192 -> 8192 23.6 and 25.1, 16384 -> 8192 44.3 and 40.6; twelve 22.1 and 25.0, 41.6 and 39.8; nine rows
+// 16384 -> 8192 37.6 and 43.1, 16384 -> 16384 70.7 and 69.6).  The gated pair, whose tiles of 64 rows of x multiply twice as much for nothing, has no such size (16 rows 4096 -> 6144 17.5 and 20.8,
+// codes 19.9 and 19.5; 8192 -> 16384 63 and 61, codes 65.9 and 66.8).
 bool by_rows(const ProductShape& s)
 {
     if (!product_tiles_fit(s)) return true;
-    const long long weights = (long long)s.in * s.out * (s.kind == kLinear ? 1 : 2);
-    return s.rows <= 8 || (s.rows <= kRows && (s.out_type == kF32 || weights < 48ll << 20));
+    return s.rows <= 8 || (s.rows <= kRows && (s.kind != kLinear || s.out_type == kF32 || (long long)s.in * s.out * s.rows < 5ll << 28));
 }
 
 // The workspace: slices' sums of the tiles; h in fp32, where codes are made of it by a launch of their own.

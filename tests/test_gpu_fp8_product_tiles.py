@@ -104,3 +104,9 @@ def test_gated_backward(torch, rows, k, n, squares):
                     assert torch.equal(out[:, :2 * n], torch.cat((dh.float() * v.float(), dh.float() * g.float()), dim=1).to(t))
                 else:
                     assert near(out[:, :2 * n], torch.cat((dg, du), dim=1), off, kind)
+
+
+# (nine to sixteen rows: below 1.25 * 2^30 products the kernel of few rows, tiles above)
+@pytest.mark.parametrize("rows,k,n", [(9, 8200, 8190), (16, 8200, 8190), (12, 16200, 8190), (16, 16200, 8190), (9, 16200, 16400)])
+def test_sixteen_rows_of_many_weights(torch, rows, k, n):
+    test_linear(torch, rows, k, n, True)

@@ -624,9 +624,11 @@ patdnn_status_t patdnn_rms_norm_backward(const patdnn_rms_desc_t* desc, const vo
                                          const float* gamma, void* dx, float* dgamma, float* workspace, size_t workspace_floats, void* stream);
 
 /*
- * Products of fp8 codes, summed in fp32.  x: codes [rows][in_features] with blocks along the rows.  Results in fp32 have fp32's precision (values below
- * 2^-126 keep what bfloat16's subnormals hold of them); those of more than a few rows in fewer bits come from the fp8 matrix instruction, which cuts off what lies below 2^-13
- * of the power of two of the largest of eight neighbouring products (1.5e-5 of a sum of normal values), and are faster.
+ * Products of fp8 codes, summed in fp32.  x: codes [rows][in_features] with blocks along the rows.
+ * Results in fp32, and those of any type of up to eight rows (16, but for large linear layers), have fp32's precision: values below 2^-126 keep what bfloat16's subnormals
+ * hold of them, and a value of 2^128 (the lowest value of fp32 or bfloat16, quantised) is infinite.  Results of more rows in fewer bits come from the fp8 matrix instruction, which is faster
+ * and cuts off what lies below 2^-13 of the power of two of the largest of eight neighbouring products: 1.5e-5 of a sum of normal values.  Within that, a row's result in 16 or 8 bits
+ * depends on how many rows share its call.  Where it must not, ask for fp32, and convert or quantise that: these sums differ by the order of their additions only.
  *   patdnn_fp8_linear          out[m][n] = act(bias[n] + sum over k of x[m][k] w[n][k])
  *   patdnn_fp8_gated           g = sum of x gate, u = sum of x up;  out = act(g) u
  *   patdnn_fp8_gated_backward  from dh, the gradient of that result:  dgate = dh u act'(g),  dup = dh act(g)   (ReLU: act' is 0 where g <= 0); the

@@ -7,7 +7,8 @@
 // rows, so that a column's codes are eight neighbouring bytes of it when the matrix is turned; turned bytes go through LDS, and rows of 128
 // bytes leave it.
 //
-// 12288 x 4096 bf16, squares, turned: 33 us, 4.5 TB/s; back to bf16 29.5 us, 5.1 TB/s.  8111 x 4500 bf16, turned: 28 us, 3.9 TB/s (its rows begin inside cache lines).
+// From memory: 16384 x 4096 bf16, blocks along the rows: 39.5 us, 5.1 TB/s (fp32 61 us, 5.5).  12288 x 4096 bf16, squares: 33 us, 4.6 TB/s; turned: 36 us, 4.2 TB/s; back to bf16
+// 37 us, 4.1 TB/s (29.5 of codes that have just been written).  8111 x 4500 bf16, turned: 30.5 us, 3.6 TB/s (its rows begin inside cache lines).
 #include "fp8.hpp"
 #include "kernels.hpp"
 #include "operators.hpp"

@@ -1,13 +1,13 @@
 // Products of fp8 codes, few rows of x: linear layers, and the gated pair of projections with its gradients.
 //
 // sum over k of x[m][k] w[n][k], 16 rows of 128 codes with 16 others at a time; sums are fp32.  There is time for the bfloat16 instructions, so sums have fp32's precision
-// whatever the result's type (1 x 12288 -> 4096 11.2 us with the fp8 instruction, 11.1 so).
+// whatever the result's type (1 x 12288 -> 4096, three matrices in turn, which the last-level cache holds: 11.2 us with the fp8 instruction, 11.1 so).
 // The weights are the first operand, so that a lane's four results are neighbours along n.
 //
 // The weights' bytes count, and every CU should have loads on their way all the time.  A workgroup takes 16 outputs (of both projections); its wavefronts take
 // pieces of 128 values of k in turn, straight from memory to registers, and add their sums up in LDS, in their order.
 //
-// From memory: 1 x 12288 -> 4096 12.7 us, 4.0 TB/s of weights; gated 1 x 4096 -> 12288 21.9 us, 4.6 TB/s.
+// From memory (twenty matrices in turn): 1 x 12288 -> 4096 12.1 us, 4.2 TB/s of weights, eight rows 14.9; gated 1 x 4096 -> 12288 21.1 us, 4.8 TB/s, codes 23.1.
 #include "fp8_products.hpp"
 
 namespace patdnn {

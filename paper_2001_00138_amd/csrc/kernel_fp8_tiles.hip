@@ -10,8 +10,8 @@
 // results for four tiles are sixteen neighbouring outputs.  For the gated pair, each 64 rows of the first projection's are followed by the same 64 of the second's,
 // so that one lane has both sums of an output, and a workgroup whose result is codes all 128 outputs that share a scale.
 //
-// 8192 x 8192 values, 8192 outputs, bf16: 407 us, 2.70 PFLOP/s (335 without the fetches); the matrix cores are busy 64 % of the cycles, at 1.69 GHz of 2.4.  fp32: 880 us.
-// Gated, 8192 x 4096 -> 12288: codes 650 us, bf16 640; its gradients 785.
+// 8192 x 8192 values, 8192 outputs, bf16: 424 to 515 us by the card's clock, 465 (2.36 PFLOP/s) in the middle of a series; the matrix cores are busy 64 % of its 818 thousand cycles.
+// (In the shortest series 407, and 335 there without the fetches.)  fp32: 890 to 910 us.  Gated, 8192 x 4096 -> 12288: codes 680 to 745 us, bf16 710, fp32 1490; its gradients in bf16 785 to 830.
 #include "fp8_products.hpp"
 
 namespace patdnn {

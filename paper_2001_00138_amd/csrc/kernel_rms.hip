@@ -9,7 +9,7 @@
 // results repeat bit for bit.  Backward, a workgroup takes several rows, a stride apart, and keeps its sums of dgamma in registers; they are
 // joined, again in a fixed order, by a second launch.
 //
-// 16384 x 4096 bf16 (from memory): codes with the residual 93 us, 5.0 TB/s; backward 109 us with its joining, 4.9 TB/s.
+// 16384 x 4096 bf16 (from memory): codes with the residual 105 us, 4.5 TB/s; backward 112 us with its joining, 4.8 TB/s, 103 without gamma's gradient.
 #include "fp8.hpp"
 #include "kernels.hpp"
 #include "operators.hpp"

@@ -604,8 +604,8 @@ patdnn_status_t patdnn_fp8_dequantize(const uint8_t* codes, const uint8_t* scale
  *   workspace          patdnn_rms_norm_workspace_floats floats for the backward call with dgamma, contents undefined before and after
  * Strides in elements between rows, values of a row adjacent (inputs >= 0, outputs >= cols).  Squares are added in fp32, in units that hold them: only a row with a
  * mean square beyond its range has rstd 0, and only one whose rstd is (a row of zeros and eps 0) has infinity.  Results repeat bit for bit.  rows == 0 is a no-op but for dgamma.  PATDNN_EUNSUPPORTED beyond 2^31 - 8321 columns (backward 2^26 - 1024)
- * and, forward, beyond what a grid of fewer than 2^32 threads holds: 2^28 - 16 rows of up to 128 columns (16 threads a row), 2^22 - 1 rows of 8192 and more (1024 threads),
- * in proportion between.
+ * and, forward, beyond what a grid of fewer than 2^32 threads holds: up to 128 columns have 16 threads a row, more have up to 1024, so the most rows are 2^28 - 16, and
+ * 2^22 - 1 are taken at any length.
  */
 typedef struct {
     int32_t rows, cols;
